@@ -334,6 +334,86 @@ int hbsjd_bikl(hbsjd_ctx *c, const float *logits_s, const float *logits_t, int r
 int hbsjd_score(hbsjd_ctx *student, hbsjd_ctx *teacher, int batch, const int32_t *tokens, const int32_t *prefix_len,
                 const int32_t *class_labels, float *bikl_pos, float *per_image, float *loss);
 
+/* ---- operators on rows of logits ------------------------------------------------------------------------------------
+ * What the distillation loop does with logits next to the rollout: rules in front of the sampler, the teacher's distribution
+ * as a list of its largest logits, and divergences with their gradients (the score above is a value only).
+ *   - They take no context: a stream (cudaStream_t as void*) of the current device, a descriptor and DEVICE pointers.
+ *   - They launch one kernel and return; results are there when the stream has got that far.  They keep nothing between
+ *     calls and allocate nothing: any number of calls may run at once, and a call may be captured into a CUDA graph.
+ *   - Rows lie ld elements apart, any ld >= V (for what is only read: any ld >= 0; 0 is one row for all).  Pointers are
+ *     aligned to their elements; rows that start on 16 bytes and arrays alike in that are fastest.
+ *   - An array that is written may be one that is read (same pointer, stride and type); else they do not overlap.
+ *   - 1 <= V <= 131072, 0 <= rows < 2^27; rows = 0 does nothing.  Element types are HBSJD_DTYPE_*; arithmetic is fp32,
+ *     bf16 results are rounded once.
+ *   - Errors: HBSJD_EINVAL (nothing was launched), HBSJD_ECUDA.  hbsjd_last_error(NULL) tells the calling thread the
+ *     details of its last failed one. */
+
+/* Rules on logits in front of hbsjd_probs / hbsjd_verify (Sec. 4.2 "verification uses the fused guided logits").  Entry v of row r:
+ *   x = logits, or guided: logits_u + cfg_scale (logits - logits_u);
+ *   n = occurrences of v among the first history_len[r] tokens of the row's history; n > 0:
+ *       x = x > 0 ? x / repetition : x * repetition;  x -= n frequency + presence;
+ *   x += bias[v];  x = -inf where the row's mask has bit v = 0, and where x is NaN (guidance of two masked branches).
+ *   logits, out [rows, V];  logits_u [rows, V] or NULL
+ *   bias         fp32 [V] or NULL
+ *   mask         uint32 [masks, ld_mask] or NULL: bit v & 31 of word v >> 5 allows v; ld_mask >= (V + 31) / 32 words
+ *   mask_row     int32 [rows] or NULL (all 0): the row's mask; a number outside 0..masks-1: none
+ *   history      int32 [sequences, ld_history] or NULL: tokens; those outside 0..V-1 are passed over
+ *   history_row  int32 [rows] or NULL (row r: sequence r, sequences >= rows); a number outside 0..sequences-1: none.  The
+ *                windows of an image share its sequence, with a longer history_len from position to position.
+ *   history_len  int32 [rows] or NULL (all history_cap): taken as 0..history_cap */
+typedef struct {
+    int32_t rows, V, dtype, masks, sequences, history_cap;
+    int64_t ld, ld_u, ld_out, ld_mask, ld_history;
+    float cfg_scale, repetition, frequency, presence;   /* repetition > 0; 1, 0, 0: no penalty */
+} hbsjd_adjust_desc;
+int hbsjd_adjust_logits(void *cuda_stream, const hbsjd_adjust_desc *d, const void *logits, const void *logits_u,
+                        const float *bias, const uint32_t *mask, const int32_t *mask_row, const int32_t *history,
+                        const int32_t *history_row, const int32_t *history_len, void *out);
+
+/* The k largest logits of every row and the mass of all others.
+ *   values  fp32 [rows, k]  the logits, largest first;  indices int32 [rows, k]  their tokens; equal logits: the lowest
+ *           token first.  -inf and NaN are no entries: where a row has fewer than k others, it ends in (-inf, -1).
+ *   rest    fp32 [rows] or NULL: log of the sum of e^{logit / temperature} over the entries that are not listed (-inf: none)
+ * 1 <= k <= min(V, 1024). */
+typedef struct {
+    int32_t rows, V, dtype, k;
+    int64_t ld;
+    float temperature;
+    uint32_t reserved;
+} hbsjd_topk_desc;
+int hbsjd_topk_logits(void *cuda_stream, const hbsjd_topk_desc *d, const void *logits, float *values, int32_t *indices,
+                      float *rest);
+
+/* Divergence of the student's distribution q = softmax(logits_s / temperature) from the teacher's p and its gradient:
+ *   loss[r] = forward KL(p || q) + reverse KL(q || p);   grad[r] = weight[r] d loss[r] / d logits_s[r]
+ * forward = reverse = 1/2 at temperature 1 is Eq. 3, as hbsjd_bikl computes it.
+ *   logits_s [rows, V] of type dtype_s;  grad [rows, V] of the same type, or NULL (loss only)
+ *   weight   fp32 [rows] or NULL (all 1): a row's weight in the total, e.g. 1 / positions.  0 leaves the row out: it is not
+ *            read, its loss is 0 and its gradient zeros
+ *   loss     fp32 [rows] or NULL
+ * An entry of -inf has no mass, neither has one whose share is below 2^-126.  Where the divergence is infinite (the student has
+ * no mass where the teacher has: forward; the other way: reverse) so is the loss; the gradient of KL(p || q) is q - p all the
+ * same, that of KL(q || p) is then not defined.  A row without mass on one side has loss 0 and gradient 0.  NaN and +inf
+ * make the row's loss and gradient NaN.
+ *
+ * hbsjd_distill: p = softmax(logits_t / temperature), logits_t [rows, V] of type dtype_t.
+ *
+ * hbsjd_distill_topk: the teacher as hbsjd_topk_logits lists it, values and indices [rows, k], 1 <= k <= 1024.  Entries
+ * with a value of -inf, a token outside 0..V-1, or a token that an earlier entry of the row has, count for nothing.
+ *   rest fp32 [rows]: all tokens that are not listed are one outcome, of mass e^rest beside the e^{value / temperature} of
+ *                     those listed (same temperature); both divergences are over these k + 1 outcomes
+ *   rest NULL:        the teacher is what is listed, renormalised; reverse has to be 0 */
+typedef struct {
+    int32_t rows, V, dtype_s, dtype_t, k, reserved;
+    int64_t ld_s, ld_t, ld_grad;
+    float temperature, forward, reverse;   /* forward, reverse >= 0 */
+    uint32_t reserved2;
+} hbsjd_distill_desc;
+int hbsjd_distill(void *cuda_stream, const hbsjd_distill_desc *d, const void *logits_s, const void *logits_t,
+                  const float *weight, float *loss, void *grad);
+int hbsjd_distill_topk(void *cuda_stream, const hbsjd_distill_desc *d, const void *logits_s, const float *values,
+                       const int32_t *indices, const float *rest, const float *weight, float *loss, void *grad);
+
 /* Per-kernel-class timing with CUDA events on the context's stream (off by default).  While enabled,
  * every launch of a timed class is bracketed by an event pair; totals accumulate until the next
  * hbsjd_profile(c, 1), which also resets them.  work = algorithmic FLOPs (GEMM: 2 M N K per launch) or
@@ -362,7 +442,7 @@ int hbsjd_profile_read(hbsjd_ctx *c, hbsjd_kernel_profile *out);
 int hbsjd_profile_launch_floor(hbsjd_ctx *c, int reps, float *us_out);
 
 const char *hbsjd_strerror(int code);
-const char *hbsjd_last_error(const hbsjd_ctx *c);
+const char *hbsjd_last_error(const hbsjd_ctx *c);   /* NULL: of the calling thread's last failed call without a context */
 
 #ifdef __cplusplus
 }

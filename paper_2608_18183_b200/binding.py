@@ -21,7 +21,7 @@ EXPORTS = ["hbsjd_create", "hbsjd_rollout", "hbsjd_prefill_passes", "hbsjd_rollo
            "hbsjd_set_state", "hbsjd_debug_read", "hbsjd_debug_forward", "hbsjd_debug_gemm",
            "hbsjd_debug_shuffle_pages", "hbsjd_debug_fold_norm", "hbsjd_debug_fail_round",
            "hbsjd_debug_force_tile", "hbsjd_gemm", "hbsjd_bikl", "hbsjd_score", "hbsjd_strerror",
-           "hbsjd_last_error"]
+           "hbsjd_last_error", "hbsjd_adjust_logits", "hbsjd_topk_logits", "hbsjd_distill", "hbsjd_distill_topk"]
 
 
 class hbsjd_model_desc(C.Structure):
@@ -61,6 +61,23 @@ class hbsjd_verify_desc(C.Structure):
                 ("batch", "window", "T", "V", "branches", "history_offset", "greedy", "top_k")] + [
                    ("cfg_scale", C.c_float), ("temperature", C.c_float), ("seed", C.c_uint64),
                    ("round", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class hbsjd_adjust_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "V", "dtype", "masks", "sequences", "history_cap")] + [
+        (n, C.c_int64) for n in ("ld", "ld_u", "ld_out", "ld_mask", "ld_history")] + [
+            (n, C.c_float) for n in ("cfg_scale", "repetition", "frequency", "presence")]
+
+
+class hbsjd_topk_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "V", "dtype", "k")] + [("ld", C.c_int64), ("temperature", C.c_float),
+                                                                        ("reserved", C.c_uint32)]
+
+
+class hbsjd_distill_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "V", "dtype_s", "dtype_t", "k", "reserved")] + [
+        (n, C.c_int64) for n in ("ld_s", "ld_t", "ld_grad")] + [
+            (n, C.c_float) for n in ("temperature", "forward", "reverse")] + [("reserved2", C.c_uint32)]
 
 
 class HbsjdError(RuntimeError):
@@ -113,6 +130,10 @@ def load():
         L.hbsjd_debug_force_tile.argtypes = [vp, C.c_int]
         L.hbsjd_bikl.argtypes = [vp, vp, vp, C.c_int, vp]
         L.hbsjd_score.argtypes = [vp, vp, C.c_int, vp, vp, vp, vp, vp, C.POINTER(C.c_float)]
+        L.hbsjd_adjust_logits.argtypes = [vp, C.POINTER(hbsjd_adjust_desc)] + [vp] * 9
+        L.hbsjd_topk_logits.argtypes = [vp, C.POINTER(hbsjd_topk_desc)] + [vp] * 4
+        L.hbsjd_distill.argtypes = [vp, C.POINTER(hbsjd_distill_desc)] + [vp] * 5
+        L.hbsjd_distill_topk.argtypes = [vp, C.POINTER(hbsjd_distill_desc)] + [vp] * 7
         L.hbsjd_strerror.argtypes = [C.c_int]
         L.hbsjd_strerror.restype = C.c_char_p
         L.hbsjd_last_error.argtypes = [vp]
@@ -141,6 +162,176 @@ def hbsjd_verify_static(stream, desc, logits, q_prev, p_out, cursor, seq, delta,
                                     delta.data_ptr(), qbase.data_ptr(), m_out.data_ptr())
     if rc != 0:
         raise HbsjdError(rc, "hbsjd_verify_static", load().hbsjd_strerror(rc).decode())
+
+
+# ---- operators on rows of logits (see include/hbsjd.h): functions of tensors, like the C entries without a context.
+# Tensors lie on one GPU, which need not be the current one.  A call goes to `stream`, or to the current stream of the tensors'
+# device; inputs made on another stream have to be ordered before it by the caller, and nothing waits for the result.
+
+class _Rows:
+    """One call: checks its tensors as they are passed in, then makes it on their device."""
+
+    def __init__(self, what, logits, stream):
+        import torch
+        self.torch, self.what, self.stream = torch, what, stream
+        self.types = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+        self.device = None
+        self.kept = []
+        self.rows, self.V = 0, 0
+        self.matrix(logits, "logits")
+        self.rows, self.V = logits.shape
+        if self.stream is not None and self.stream.device != self.device:
+            self.refuse(f"stream of {self.stream.device}, tensors on {self.device}")
+
+    def refuse(self, why):
+        raise HbsjdError(-1, self.what, why)
+
+    def _placed(self, x, name):
+        if not isinstance(x, self.torch.Tensor) or not x.is_cuda:
+            self.refuse(f"{name} is not a tensor on a GPU")
+        if self.device is None:
+            self.device = x.device
+        if x.device != self.device:
+            self.refuse(f"{name} lies on {x.device}, not on {self.device}")
+        self.kept.append(x)
+
+    def matrix(self, x, name, dtype=None, shape=None, written=False):
+        """(pointer, row stride, type) of rows whose elements are neighbours."""
+        self._placed(x, name)
+        if dtype is None and x.dtype not in self.types or dtype is not None and x.dtype != dtype:
+            self.refuse(f"{name} has type {x.dtype}")
+        if x.dim() != 2 or shape is not None and tuple(x.shape) != tuple(shape):
+            self.refuse(f"{name} has shape {tuple(x.shape)}" + (f", not {tuple(shape)}" if shape is not None else ""))
+        if x.shape[1] > 1 and x.stride(1) != 1:
+            self.refuse(f"{name}: the elements of a row are not neighbours")
+        ld = x.stride(0) if x.shape[0] > 1 else x.shape[1]
+        if written and ld < x.shape[1]:
+            self.refuse(f"{name}: rows overlap")
+        return x.data_ptr(), ld, self.types.get(x.dtype)
+
+    def vector(self, x, name, dtype, n):
+        if x is None:
+            return None
+        self._placed(x, name)
+        if x.dtype != dtype or tuple(x.shape) != (n,) or not x.is_contiguous():
+            self.refuse(f"{name} has to be contiguous, of type {dtype} and shape ({n},)")
+        return x.data_ptr()
+
+    def new(self, shape, dtype):
+        with self.torch.cuda.device(self.device), self.torch.cuda.stream(self.stream):
+            return self.torch.empty(shape, dtype=dtype, device=self.device)
+
+    def call(self, entry, desc, *pointers):
+        torch = self.torch
+        with torch.cuda.device(self.device):
+            stream = self.stream if self.stream is not None else torch.cuda.current_stream()
+            rc = entry(C.c_void_p(stream.cuda_stream), C.byref(desc), *pointers)
+        if rc != 0:
+            raise HbsjdError(rc, self.what, load().hbsjd_last_error(None).decode())
+        if self.stream is not None:
+            # memory that its owner gives back is not to be used again before this call has run
+            for x in self.kept:
+                x.record_stream(self.stream)
+
+
+def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=None, mask_row=None, history=None,
+                        history_row=None, history_len=None, repetition=1.0, frequency=0.0, presence=0.0, out=None,
+                        stream=None):
+    """Guidance, penalties, bias and masks on [rows, V] logits of fp32 or bf16 -> out, a new tensor or the given one (which may
+    be `logits`).  mask: int32 or uint32 words [masks, words], history: int32 [sequences, tokens], row numbers and
+    lengths int32 [rows], bias fp32 [V]."""
+    c = _Rows("hbsjd_adjust_logits", logits, stream)
+    torch, rows, V = c.torch, c.rows, c.V
+    x, ld, dtype = c.matrix(logits, "logits")
+    u, ld_u = None, 0
+    if logits_u is not None:
+        u, ld_u, _ = c.matrix(logits_u, "logits_u", logits.dtype, (rows, V))
+    words, ld_mask = None, 0
+    if mask is not None:
+        words, ld_mask, _ = c.matrix(mask, "mask", torch.uint32 if getattr(mask, "dtype", None) == torch.uint32
+                                     else torch.int32)
+        if mask.shape[1] < (V + 31) // 32:
+            c.refuse(f"mask has {mask.shape[1]} words for {V} entries")
+        if mask.shape[0] > 1 and ld_mask < mask.shape[1]:
+            c.refuse("mask: rows overlap")
+        ld_mask = max(ld_mask, mask.shape[1])
+    tok, ld_history = None, 0
+    if history is not None and history.shape[-1] > 0:
+        tok, ld_history, _ = c.matrix(history, "history", torch.int32)
+        if history.shape[0] > 1 and ld_history < history.shape[1]:
+            c.refuse("history: rows overlap")
+    if out is None:
+        out = c.new((rows, V), logits.dtype)
+    o, ld_out, _ = c.matrix(out, "out", logits.dtype, (rows, V), written=True)
+    d = hbsjd_adjust_desc(rows, V, dtype, 0 if words is None else mask.shape[0], 0 if tok is None else history.shape[0],
+                          0 if tok is None else history.shape[1], ld, ld_u, ld_out, ld_mask, ld_history, cfg_scale,
+                          repetition, frequency, presence)
+    c.call(load().hbsjd_adjust_logits, d, x, u, c.vector(bias, "bias", torch.float32, V), words,
+           c.vector(mask_row, "mask_row", torch.int32, rows), tok, c.vector(history_row, "history_row", torch.int32, rows),
+           c.vector(history_len, "history_len", torch.int32, rows), o)
+    return out
+
+
+def hbsjd_topk_logits(logits, k, temperature=1.0, want_rest=True, stream=None):
+    """The k largest logits of each row of [rows, V]: (values fp32 [rows, k], indices int32 [rows, k], rest fp32 [rows] or
+    None)."""
+    c = _Rows("hbsjd_topk_logits", logits, stream)
+    torch = c.torch
+    x, ld, dtype = c.matrix(logits, "logits")
+    if not 1 <= k <= min(c.V, 1024):
+        c.refuse(f"k = {k} is out of range")
+    values, indices = c.new((c.rows, k), torch.float32), c.new((c.rows, k), torch.int32)
+    rest = c.new((c.rows,), torch.float32) if want_rest else None
+    c.call(load().hbsjd_topk_logits, hbsjd_topk_desc(c.rows, c.V, dtype, k, ld, temperature, 0), x, values.data_ptr(),
+           indices.data_ptr(), None if rest is None else rest.data_ptr())
+    return values, indices, rest
+
+
+def _distill(c, logits_s, weight, temperature, forward, reverse, want_grad, grad, k=0, dtype_t=0, ld_t=0):
+    """Descriptor, pointers and outputs that both forms of the divergence share."""
+    torch = c.torch
+    s, ld_s, dtype_s = c.matrix(logits_s, "logits_s")
+    if want_grad and grad is None:
+        grad = c.new((c.rows, c.V), logits_s.dtype)
+    g, ld_g = None, 0
+    if grad is not None:
+        g, ld_g, _ = c.matrix(grad, "grad", logits_s.dtype, (c.rows, c.V), written=True)
+    w = c.vector(weight, "weight", torch.float32, c.rows)
+    loss = c.new((c.rows,), torch.float32)
+    d = hbsjd_distill_desc(c.rows, c.V, dtype_s, dtype_t, k, 0, ld_s, ld_t, ld_g, temperature, forward, reverse, 0)
+    return d, s, w, loss, grad, g
+
+
+def hbsjd_distill(logits_s, logits_t, weight=None, temperature=1.0, forward=0.5, reverse=0.5, want_grad=True, grad=None,
+                  stream=None):
+    """forward KL(p || q) + reverse KL(q || p) of each row of the student's [rows, V] logits (q) against the teacher's (p), and
+    weight times its gradient in logits_s: (loss fp32 [rows], grad like logits_s or None).  The defaults are Eq. 3.
+    grad: a tensor for the gradient, which may be logits_s.  In a training step: logits_s.backward(grad)."""
+    c = _Rows("hbsjd_distill", logits_s, stream)
+    t, ld_t, dtype_t = c.matrix(logits_t, "logits_t", None, (c.rows, c.V))
+    d, s, w, loss, grad, g = _distill(c, logits_s, weight, temperature, forward, reverse, want_grad, grad,
+                                      dtype_t=dtype_t, ld_t=ld_t)
+    c.call(load().hbsjd_distill, d, s, t, w, loss.data_ptr(), g)
+    return loss, grad
+
+
+def hbsjd_distill_topk(logits_s, values, indices, rest=None, weight=None, temperature=1.0, forward=1.0, reverse=0.0,
+                       want_grad=True, grad=None, stream=None):
+    """hbsjd_distill against a teacher that is given by its largest logits: values fp32 and indices int32 [rows, k], rest fp32
+    [rows] (the tokens that are not listed as one outcome) or None (renormalised over the list)."""
+    c = _Rows("hbsjd_distill_topk", logits_s, stream)
+    torch = c.torch
+    if not isinstance(values, torch.Tensor) or values.dim() != 2:
+        c.refuse("values is not a matrix")
+    k = values.shape[1]
+    for x, name, dtype in ((values, "values", torch.float32), (indices, "indices", torch.int32)):
+        c.matrix(x, name, dtype, (c.rows, k))
+        if not x.is_contiguous():
+            c.refuse(f"{name} is not contiguous")
+    r = c.vector(rest, "rest", torch.float32, c.rows)
+    d, s, w, loss, grad, g = _distill(c, logits_s, weight, temperature, forward, reverse, want_grad, grad, k=k)
+    c.call(load().hbsjd_distill_topk, d, s, values.data_ptr(), indices.data_ptr(), r, w, loss.data_ptr(), g)
+    return loss, grad
 
 
 class Context:

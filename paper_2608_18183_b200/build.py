@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIBDIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIBDIR, "libhbsjd.so")
 SOURCES = ["api.cu", "model_kernels.cu", "state_kernels.cu", "gemm_tcgen05.cu", "gemm_skinny.cu", "attention_tma.cu", "score_kernels.cu",
-           "accept_persistent.cu"]
+           "accept_persistent.cu", "distill_kernels.cu", "topk_kernels.cu", "adjust_kernels.cu", "logits_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler",
               "-fPIC", "--use_fast_math=false"]
 

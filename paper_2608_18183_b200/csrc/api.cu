@@ -867,7 +867,7 @@ const char* hbsjd_strerror(int code) {
     }
 }
 
-const char* hbsjd_last_error(const hbsjd_ctx* c) { return c ? c->err : "null context"; }
+const char* hbsjd_last_error(const hbsjd_ctx* c) { return c ? c->err : last_detail(); }
 
 int hbsjd_create(hbsjd_ctx** out, const hbsjd_model_desc* m, const void* weights, size_t weight_bytes,
                  int max_batch, int max_window, void* cuda_stream) {

@@ -205,4 +205,7 @@ int gemm_tcgen05_qkv(const bf16* A, const bf16* Wqkv, bf16* q, const State& st, 
                      const float* rope_cs, const KvView& kv, int m_cap, const NormIn& nin, int32_t* error_flag,
                      Stream& s, char* err, size_t errlen, int tile = 0);
 
+// ---- operators on rows of logits (logits_api.cu)
+const char* last_detail();  // of the calling thread's last failed call
+
 }  // namespace hbsjd
