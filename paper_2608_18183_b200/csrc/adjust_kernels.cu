@@ -14,32 +14,59 @@ namespace hbsjd {
 namespace {
 
 constexpr int AD_THREADS = 256;
+constexpr int AD_GROUPS = 4;  // 16-byte groups of a thread: all of a CTA's logits are on their way while it counts the history
 
-struct Rules {
-    const AdjustArgs& a;
-    const uint32_t* bits;   // the row's mask, or null
-    const int32_t* counts;  // shared: occurrences of the chunk's tokens, or null
-    template <int N>
-    __device__ __forceinline__ void apply(float (&x)[N], const float (&u)[N], int v, int e, int limit) const {
+// x[i] is entry v + i of the row; those outside [0, V) are not looked at (v may be negative).
+template <int G>
+__device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t* bits, const int32_t* counts, float (&x)[G], int v,
+                                            int e) {
+    if (counts) {
+        int n[G];
+        bool any = false;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (v + i < 0 || v + i >= limit) continue;
-            if (a.u) x[i] = fmaf(a.cfg_scale, x[i] - u[i], u[i]);
-            if (counts) {
-                const int n = counts[e + i];
-                if (n) {
+        for (int i = 0; i < G; i += 4) {
+            const int4 q = *reinterpret_cast<const int4*>(counts + e + i);
+            n[i] = q.x, n[i + 1] = q.y, n[i + 2] = q.z, n[i + 3] = q.w;
+            any |= (q.x | q.y | q.z | q.w) != 0;
+        }
+        if (any) {
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (n[i]) {
                     x[i] = x[i] > 0.f ? x[i] / a.repetition : x[i] * a.repetition;
-                    x[i] -= fmaf((float)n, a.frequency, a.presence);
+                    x[i] -= fmaf((float)n[i], a.frequency, a.presence);
                 }
-            }
-            if (a.bias) x[i] += __ldg(a.bias + v + i);
-            if (bits && !(__ldg(bits + ((v + i) >> 5)) >> ((v + i) & 31) & 1)) x[i] = -INFINITY;
-            if (x[i] != x[i]) x[i] = -INFINITY;
         }
     }
-};
+    if (a.bias) {
+        const float* b = a.bias + v;
+        if (v >= 0 && v + G <= a.V && ((uintptr_t)b & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < G; i += 4) {
+                const float4 q = __ldg(reinterpret_cast<const float4*>(b + i));
+                x[i] += q.x, x[i + 1] += q.y, x[i + 2] += q.z, x[i + 3] += q.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (v + i >= 0 && v + i < a.V) x[i] += __ldg(b + i);
+        }
+    }
+    if (bits) {
+        // the G bits from v on, which may lie in two words
+        const int last = (a.V - 1) >> 5, w = v >> 5;
+        const uint32_t lo = w >= 0 ? __ldg(bits + w) : 0, hi = (v & 31) + G > 32 && w < last ? __ldg(bits + w + 1) : 0;
+        const uint32_t m = __funnelshift_r(lo, hi, v & 31);
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            if (!(m >> i & 1)) x[i] = -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+        if (x[i] != x[i]) x[i] = -INFINITY;
+}
 
-template <typename T>
+template <typename T, bool GUIDED>
 __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, int chunks) {
     constexpr int G = 16 / sizeof(T);
     extern __shared__ __align__(16) unsigned char smem[];
@@ -49,70 +76,84 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
     const int64_t row = blockIdx.x / chunks;
     const int v0 = blockIdx.x % chunks * chunk, n = min(chunk, a.V - v0);
     const T* x = (const T*)a.x + row * a.ld + v0;
-    const T* u = a.u ? (const T*)a.u + row * a.ld_u + v0 : nullptr;
+    const T* u = (const T*)a.u + (GUIDED ? row * a.ld_u + v0 : 0);
     T* out = (T*)a.out + row * a.ld_out + v0;
-    const int P = phase_of(out);
-    const bool wide = phase_of(x) == P && (!u || phase_of(u) == P);
-    Rules r = {a, nullptr, nullptr};
+    // groups of 16 bytes of the output; P + n <= chunk + G - 1 elements, so a chunk of whole rounds has one group more at most
+    const int P = phase_of(out), rounds = (P + n + AD_THREADS * G - 1) / (AD_THREADS * G);
+    const bool wide = phase_of(x) == P && (!GUIDED || phase_of(u) == P);
+    float f[AD_GROUPS][G];
+#pragma unroll
+    for (int r = 0; r < AD_GROUPS; ++r) {
+        const int e = (r * AD_THREADS + tid) * G - P;
+        if (wide && e >= 0 && e + G <= n) {
+            get<G>(x + e, f[r]);
+            if (GUIDED) {
+                float g[G];
+                get<G>(u + e, g);
+#pragma unroll
+                for (int i = 0; i < G; ++i) f[r][i] = fmaf(a.cfg_scale, f[r][i] - g[i], g[i]);
+            }
+        }
+    }
+    const uint32_t* bits = nullptr;
     if (a.mask) {
         const int m = a.mask_row ? a.mask_row[row] : 0;
-        if (m >= 0 && m < a.masks) r.bits = a.mask + m * a.ld_mask;
+        if (m >= 0 && m < a.masks) bits = a.mask + m * a.ld_mask;
     }
+    const int32_t* counts = nullptr;
     if (a.history) {
         const int64_t h = a.history_row ? a.history_row[row] : row;
         const int len = min(a.history_len ? a.history_len[row] : a.history_cap, a.history_cap);
         if (h >= 0 && h < a.histories && len > 0) {
-            int32_t* counts = (int32_t*)smem;  // element P is the chunk's first
-            for (int i = tid; i < P + n; i += AD_THREADS) counts[i] = 0;
+            int32_t* count = (int32_t*)smem;  // element P is the chunk's first
+            for (int i = tid * 4; i < P + n; i += AD_THREADS * 4) *reinterpret_cast<int4*>(count + i) = make_int4(0, 0, 0, 0);
             __syncthreads();
             const int32_t* tok = a.history + h * a.ld_history;
             for (int i = tid; i < len; i += AD_THREADS) {
                 const int64_t e = (int64_t)tok[i] - v0;
-                if (e >= 0 && e < n) atomicAdd(&counts[P + e], 1);
+                if (e >= 0 && e < n) atomicAdd(&count[P + e], 1);
             }
             __syncthreads();
-            r.counts = counts;
+            counts = count;
         }
     }
-    if (wide) {
-        for (int e = tid * G; e < P + n; e += AD_THREADS * G) {
-            float f[G], g[G] = {};
-            if (e >= P && e + G <= P + n) {
-                get<G>(x + e - P, f);
-                if (u) get<G>(u + e - P, g);
-            } else {
 #pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    const bool in = e + i >= P && e + i < P + n;
-                    f[i] = in ? to_f<T>(x[e + i - P]) : 0.f;
-                    g[i] = in && u ? to_f<T>(u[e + i - P]) : 0.f;
-                }
+    for (int r = 0; r < AD_GROUPS + 1; ++r) {
+        if (r >= rounds) break;
+        const int e = (r * AD_THREADS + tid) * G - P;
+        if (e >= n) break;
+        float y[G];
+        if (r < AD_GROUPS && wide && e >= 0 && e + G <= n) {
+#pragma unroll
+            for (int i = 0; i < G; ++i) y[i] = f[r < AD_GROUPS ? r : 0][i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                const bool in = e + i >= 0 && e + i < n;
+                y[i] = in ? to_f<T>(x[e + i]) : 0.f;
+                if (GUIDED && in) y[i] = fmaf(a.cfg_scale, y[i] - to_f<T>(u[e + i]), to_f<T>(u[e + i]));
             }
-            r.apply<G>(f, g, v0 + e - P, e, v0 + n);
-            put_at<T, G>(out, e - P, n, f);
         }
-    } else {
-        for (int i = tid; i < n; i += AD_THREADS) {
-            float f[1] = {to_f<T>(x[i])}, g[1] = {u ? to_f<T>(u[i]) : 0.f};
-            r.apply<1>(f, g, v0 + i, P + i, v0 + n);
-            out[i] = from_f<T>(f[0]);
-        }
+        apply_rules<G>(a, bits, counts, y, v0 + e, P + e);
+        put_at<T, G>(out, e, n, y);
     }
 }
 
-template <typename T>
+template <typename T, bool GUIDED>
 cudaError_t run_adjust(const AdjustArgs& a, int rows, Stream& s) {
-    int chunk = 8192;
-    while (chunk > 1024 && (int64_t)rows * ((a.V + chunk - 1) / chunk) < 2 * device_sm_count()) chunk /= 2;
+    constexpr int G = 16 / sizeof(T);
+    int chunk = AD_THREADS * G * AD_GROUPS;
+    while (chunk > AD_THREADS * G && (int64_t)rows * ((a.V + chunk - 1) / chunk) < 2 * device_sm_count()) chunk /= 2;
     const int chunks = (a.V + chunk - 1) / chunk;
-    const size_t smem = a.history ? (min(chunk, a.V) + 8) * sizeof(int32_t) : 0;
-    return launch_k(k_adjust<T>, dim3((unsigned)rows * chunks), dim3(AD_THREADS), smem, s, a, chunk, chunks);
+    const size_t smem = a.history ? (min(chunk, a.V) + 16) * sizeof(int32_t) : 0;
+    return launch_k(k_adjust<T, GUIDED>, dim3((unsigned)rows * chunks), dim3(AD_THREADS), smem, s, a, chunk, chunks);
 }
 
 }  // namespace
 
 cudaError_t launch_adjust(const AdjustArgs& a, int rows, int dtype, Stream& s) {
-    return dtype ? run_adjust<bf16>(a, rows, s) : run_adjust<float>(a, rows, s);
+    if (a.u) return dtype ? run_adjust<bf16, true>(a, rows, s) : run_adjust<float, true>(a, rows, s);
+    return dtype ? run_adjust<bf16, false>(a, rows, s) : run_adjust<float, false>(a, rows, s);
 }
 
 }  // namespace hbsjd

@@ -3,8 +3,7 @@
 // With x = s / tau, y = t / tau, q = softmax(x), p = softmax(y), d = x - y and delta = log sum e^x - log sum e^y:
 //   KL(p || q) = delta - E_p d,    KL(q || p) = E_q d - delta,
 //   d KL(p || q) / dx = q - p,     d KL(q || p) / dx = q (d - E_q d),
-// so five sums over the row (two of exponentials, two weighted by d, and their maxima) give the loss, and a second look at the
-// row the gradient.  The row stays in shared memory between the two: it is read from HBM once, the gradient written once, and
+// so four sums over the row (two of exponentials, two weighted by d) give the loss, and a second look at the row the gradient.  The row stays in shared memory between the two: it is read from HBM once, the gradient written once, and
 // those 12 V bytes (two fp32 rows) are what bounds the kernel.  Rows that a CTA cannot hold beside others are split over a
 // cluster, whose CTAs exchange the sums through distributed shared memory; so are few rows, to use more SMs.
 #include "logit_rows.cuh"
@@ -26,6 +25,7 @@ __global__ void __launch_bounds__(THREADS) k_distill(DistillArgs a) {
     constexpr int G = sizeof(TS) == 2 && sizeof(TT) == 2 ? 8 : 4;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Slots<Pair, THREADS> slots;
+    __shared__ int special;  // a logit of the slice asks for care
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x;
@@ -44,38 +44,71 @@ __global__ void __launch_bounds__(THREADS) k_distill(DistillArgs a) {
     const int P = common_phase(s, t), groups = (P + n + G - 1) / G;
     TS* ss = (TS*)smem;
     TT* st = (TT*)(smem + (a.slice + 16) * sizeof(TS));
-    stage_row<TS, G, THREADS>(ss, s, n, P);
-    stage_row<TT, G, THREADS>(st, t, n, P);
+    stage_row<TS, G, THREADS>(ss, s, n, P, PAD);
+    stage_row<TT, G, THREADS>(st, t, n, P, PAD);
+    if (tid == 0) special = 0;
     cp_async_wait_all();
     __syncthreads();
 
     const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
-    float ms = -INFINITY, mt = -INFINITY;
-    for (int j = tid; j < groups; j += THREADS) {
+    // A warp sums against the largest logits of its first groups.  That overflows, or meets what has no finite difference, in few
+    // rows; their warps find their maxima and look at every entry.
+    Pair v = Pair::none();
+    {
         float x[G], y[G];
-        get<G>(ss + j * G, x);
-        get<G>(st + j * G, y);
+        if (tid < groups) {
+            get<G>(ss + tid * G, x);
+            get<G>(st + tid * G, y);
 #pragma unroll
-        for (int i = 0; i < G; ++i) ms = fmaxf(ms, x[i]), mt = fmaxf(mt, y[i]);
-    }
-    // (x - m before the product: a row of the lowest finite value is uniform)
-    const float os = ms == -INFINITY ? 0.f : ms, ot = mt == -INFINITY ? 0.f : mt;
-    Pair v = {ms, 0.f, 0.f, mt, 0.f, 0.f};
-    for (int j = tid; j < groups; j += THREADS) {
-        float x[G], y[G];
-        get<G>(ss + j * G, x);
-        get<G>(st + j * G, y);
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-            const float xo = x[i] - os, yo = y[i] - ot, es = ex2(xo * c), et = ex2(yo * c), d = xo - yo;
-            v.zs += es;
-            v.zt += et;
-            // no mass, no share: d is infinite or NaN where one or both are masked
-            v.as += es == 0.f ? 0.f : es * d;
-            v.at += et == 0.f ? 0.f : et * d;
+            for (int i = 0; i < G; ++i)
+                if (tid * G + i >= P && tid * G + i < P + n) v.ms = fmaxf(v.ms, x[i]), v.mt = fmaxf(v.mt, y[i]);
         }
+        v.share();
+        const f32x2 os = both(-v.ms), ot = both(-v.mt), c2 = both(c), minus = both(-1.f);
+        f32x2 zs = both(0.f), zt = zs, as = zs, at = zs;
+        for (int j = tid; j < groups; j += THREADS) {
+            get<G>(ss + j * G, x);
+            get<G>(st + j * G, y);
+#pragma unroll
+            for (int i = 0; i < G; i += 2) {
+                const f32x2 xo = add2(both(x[i], x[i + 1]), os), yo = add2(both(y[i], y[i + 1]), ot);
+                const f32x2 es = ex2(mul2(xo, c2)), et = ex2(mul2(yo, c2)), d = fma2(yo, minus, xo);
+                zs = add2(zs, es);
+                zt = add2(zt, et);
+                as = fma2(es, d, as);
+                at = fma2(et, d, at);
+            }
+        }
+        v.zs = sum_of_warp(sum2(zs));
+        v.zt = sum_of_warp(sum2(zt));
+        v.as = sum_of_warp(sum2(as));
+        v.at = sum_of_warp(sum2(at));
     }
-    v = merge_warp(v, c);
+    // (false for NaN, infinities, and sums that a factor could not bring down again)
+    if (!(v.zs < 1e12f && v.zs > 0.f && v.zt < 1e12f && v.zt > 0.f && fabsf(v.as) < 1e30f && fabsf(v.at) < 1e30f)) {
+        const bool any = (tid & ~31) < groups;
+        if (any) special = 1;
+        v = Pair::none();
+        for (int j = tid; j < groups; j += THREADS)
+            for (int e = max(j * G, P); e < min(j * G + G, P + n); ++e)
+                v.ms = fmaxf(v.ms, to_f<TS>(ss[e])), v.mt = fmaxf(v.mt, to_f<TT>(st[e]));
+        v.share();
+        const float os = v.ms == -INFINITY ? 0.f : v.ms, ot = v.mt == -INFINITY ? 0.f : v.mt;
+        for (int j = tid; j < groups; j += THREADS)
+            for (int e = max(j * G, P); e < min(j * G + G, P + n); ++e) {
+                // (x - m before the product: a row of the lowest finite value is uniform)
+                const float xo = to_f<TS>(ss[e]) - os, yo = to_f<TT>(st[e]) - ot, es = ex2(xo * c), et = ex2(yo * c);
+                v.zs += es;
+                v.zt += et;
+                // no mass, no share: d is infinite or NaN where one or both are masked
+                v.as += es == 0.f ? 0.f : es * (xo - yo);
+                v.at += et == 0.f ? 0.f : et * (xo - yo);
+            }
+        v.zs = sum_of_warp(v.zs);
+        v.zt = sum_of_warp(v.zt);
+        v.as = sum_of_warp(v.as);
+        v.at = sum_of_warp(v.at);
+    }
     if (a.ctas > 1) cluster_wait();  // every CTA of the row runs
     post(v, slots, a.ctas);
     posted(a.ctas);
@@ -99,19 +132,29 @@ __global__ void __launch_bounds__(THREADS) k_distill(DistillArgs a) {
     }
     // w / tau (a (q - p) + b q (d - E_q d)) = q (k0 + k1 d) - k2 p
     const float f = w * inv_tau;
-    const bool both = a.reverse != 0.f;
-    const float k0 = f * (both ? a.forward - a.reverse * A_q : a.forward), k1 = f * a.reverse * inv_tau, k2 = f * a.forward;
+    const bool rev = a.reverse != 0.f;
+    const float k0 = f * (rev ? a.forward - a.reverse * A_q : a.forward), k1 = f * a.reverse * inv_tau, k2 = f * a.forward;
     const int Pg = phase_of(g) % G;  // the gradient is written wide, whatever the others' alignment
     const bool wide = P % G == Pg;
+    if (special) {
+        for (int e = tid; e < n; e += THREADS) {
+            const float xo = to_f<TS>(ss[P + e]) - v.ms, yo = to_f<TT>(st[P + e]) - v.mt;
+            const float q = ex2(fmaf(xo, c, -ls)), p = ex2(fmaf(yo, c, -lt)), k = rev ? fmaf(k1, xo - yo, k0) : k0;
+            g[e] = from_f<TS>(fmaf(-k2, p, q == 0.f ? 0.f : q * k));
+        }
+        return;
+    }
+    const f32x2 os = both(-v.ms), ot = both(-v.mt), c2 = both(c), minus = both(-1.f), nls = both(-ls), nlt = both(-lt);
+    const f32x2 K0 = both(k0), K1 = both(k1), K2 = both(-k2);
     for (int e = tid * G - Pg; e < n; e += THREADS * G) {
         float x[G], y[G];
         get_at<TS, G>(ss, P, e, n, wide, x);
         get_at<TT, G>(st, P, e, n, wide, y);
 #pragma unroll
-        for (int i = 0; i < G; ++i) {
-            const float xo = x[i] - v.ms, yo = y[i] - v.mt, q = ex2(fmaf(xo, c, -ls)), p = ex2(fmaf(yo, c, -lt));
-            const float k = both ? fmaf(k1, xo - yo, k0) : k0;
-            x[i] = fmaf(-k2, p, q == 0.f ? 0.f : q * k);
+        for (int i = 0; i < G; i += 2) {
+            const f32x2 xo = add2(both(x[i], x[i + 1]), os), yo = add2(both(y[i], y[i + 1]), ot);
+            const f32x2 q = ex2(fma2(xo, c2, nls)), p = ex2(fma2(yo, c2, nlt)), k = fma2(K1, fma2(yo, minus, xo), K0);
+            split(fma2(K2, p, mul2(q, k)), x[i], x[i + 1]);
         }
         put_at<TS, G>(g, e, n, x);
     }
@@ -124,7 +167,7 @@ __device__ __forceinline__ float log_add(float x, float y) {
 }
 
 template <typename TS, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_distill_topk(DistillArgs a) {
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_distill_topk(DistillArgs a) {
     constexpr int G = 16 / sizeof(TS);
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Slots<Pair, THREADS> slots;
@@ -149,7 +192,7 @@ __global__ void __launch_bounds__(THREADS) k_distill_topk(DistillArgs a) {
     float* xk = (float*)(smem + (a.slice + 16) * sizeof(TS));  // [k] the student's logit of a listed token of the slice
     int32_t* at = (int32_t*)(xk + k);                          // [k] its place in the slice, -1: not here
     uint32_t* seen = (uint32_t*)(at + k);                      // a bit per element of the slice
-    stage_row<TS, G, THREADS>(ss, s, n, P);
+    stage_row<TS, G, THREADS>(ss, s, n, P, PAD);
 
     // while the row is on its way: which entries lie in the slice, and is a token listed twice (the first entry counts)
     const float* val = a.values + row * k;
@@ -179,35 +222,64 @@ __global__ void __launch_bounds__(THREADS) k_distill_topk(DistillArgs a) {
         }
     }
     const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
-    // listed tokens leave the slice; v: their sums, student and teacher
+    // listed tokens leave the slice; v: their sums, student and teacher (warps without any have none)
     Pair v = Pair::none();
-    for (int i = tid; i < k; i += THREADS)
-        if (at[i] >= 0) {
-            const float x = to_f<TS>(ss[P + at[i]]), y = val[i];
-            xk[i] = x;
-            ss[P + at[i]] = from_f<TS>(-INFINITY);
-            const float none = x == -INFINITY ? x : 0.f;
-            v = merge(v, {x, none ? 0.f : 1.f + (x - x), 0.f, y, 1.f + (y - y), none}, c);
-        }
+    const bool lists = (tid & ~31) < k;
+    if (lists) {
+        for (int i = tid; i < k; i += THREADS)
+            if (at[i] >= 0) {
+                const float x = to_f<TS>(ss[P + at[i]]);
+                xk[i] = x;
+                ss[P + at[i]] = from_f<TS>(-INFINITY);
+                v.ms = fmaxf(v.ms, x);
+                v.mt = fmaxf(v.mt, val[i]);
+            }
+        v.share();
+        const float os = v.ms == -INFINITY ? 0.f : v.ms, ot = v.mt == -INFINITY ? 0.f : v.mt;
+        for (int i = tid; i < k; i += THREADS)
+            if (at[i] >= 0) {
+                const float xo = xk[i] - os, yo = val[i] - ot, es = ex2(xo * c), et = ex2(yo * c);
+                v.zs += es;
+                v.zt += et;
+                v.as += es == 0.f ? 0.f : es * (xo - yo);
+                v.at += et == 0.f ? 0.f : et * (xo - yo);
+            }
+        v.zs = sum_of_warp(v.zs);
+        v.zt = sum_of_warp(v.zt);
+        v.as = sum_of_warp(v.as);
+        v.at = sum_of_warp(v.at);
+    }
     __syncthreads();
-    // u: all other tokens
-    float m = -INFINITY;
-    for (int j = tid; j < groups; j += THREADS) {
+    // u: all other tokens, against the largest of a warp's first groups; where that overflows or leaves nothing, of all of its
+    Mass u = Mass::none();
+    {
         float x[G];
-        get<G>(ss + j * G, x);
+        if (tid < groups) {
+            get<G>(ss + tid * G, x);
 #pragma unroll
-        for (int i = 0; i < G; ++i) m = fmaxf(m, x[i]);
-    }
-    const float o = m == -INFINITY ? 0.f : m;
-    Mass u = {m, 0.f};
-    for (int j = tid; j < groups; j += THREADS) {
-        float x[G];
-        get<G>(ss + j * G, x);
+            for (int i = 0; i < G; ++i)
+                if (tid * G + i >= P && tid * G + i < P + n) u.m = fmaxf(u.m, x[i]);
+        }
+        u.share();
+        const f32x2 o = both(-u.m), c2 = both(c);
+        f32x2 z = both(0.f);
+        for (int j = tid; j < groups; j += THREADS) {
+            get<G>(ss + j * G, x);
 #pragma unroll
-        for (int i = 0; i < G; ++i) u.z += ex2((x[i] - o) * c);
+            for (int i = 0; i < G; i += 2) z = add2(z, ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)));
+        }
+        u.z = sum_of_warp(sum2(z));
     }
-    v = merge_warp(v, c);
-    u = merge_warp(u, c);
+    if (!(u.z < 1e12f && u.z > 0.f)) {
+        u = Mass::none();
+        for (int j = tid; j < groups; j += THREADS)
+            for (int e = max(j * G, P); e < min(j * G + G, P + n); ++e) u.m = fmaxf(u.m, to_f<TS>(ss[e]));
+        u.share();
+        const float o = u.m == -INFINITY ? 0.f : u.m;
+        for (int j = tid; j < groups; j += THREADS)
+            for (int e = max(j * G, P); e < min(j * G + G, P + n); ++e) u.z += ex2((to_f<TS>(ss[e]) - o) * c);
+        u.z = sum_of_warp(u.z);
+    }
     if (a.ctas > 1) cluster_wait();  // every CTA of the row runs
     post(v, slots, a.ctas);
     post(u, slots_other, a.ctas);
@@ -254,11 +326,12 @@ __global__ void __launch_bounds__(THREADS) k_distill_topk(DistillArgs a) {
     k0 = u.z == 0.f ? 0.f : k0 * f / u.z;
     const float om = u.m == -INFINITY ? 0.f : u.m;
     const int Pg = phase_of(g);  // the gradient is written wide, whatever the others' alignment
+    const f32x2 o = both(-om), c2 = both(c), K0 = both(k0);
     for (int e = tid * G - Pg; e < n; e += THREADS * G) {
         float x[G];
         get_at<TS, G>(ss, P, e, n, P == Pg, x);
 #pragma unroll
-        for (int i = 0; i < G; ++i) x[i] = ex2((x[i] - om) * c) * k0;
+        for (int i = 0; i < G; i += 2) split(mul2(ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)), K0), x[i], x[i + 1]);
         put_at<TS, G>(g, e, n, x);
     }
     __syncthreads();  // the listed tokens' places were written above

@@ -24,6 +24,47 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// Two fp32 values in one register pair: sums and products of both by one instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 both(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ f32x2 both(float v) { return both(v, v); }
+__device__ __forceinline__ void split(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 ex2(f32x2 v) {
+    float lo, hi;
+    split(v, lo, hi);
+    return both(ex2(lo), ex2(hi));
+}
+__device__ __forceinline__ float sum2(f32x2 v) {
+    float lo, hi;
+    split(v, lo, hi);
+    return lo + hi;
+}
+// Largest of the warp's values that are numbers.
+__device__ __forceinline__ float max_of_warp(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
 // ------------------------------------------------------------------ clusters
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -60,11 +101,14 @@ __device__ __forceinline__ int phase_of(const T* p) {
     return (int)((reinterpret_cast<uintptr_t>(p) / sizeof(T)) % (16 / sizeof(T)));
 }
 
-// All threads: src[0, n) to dst[P, P + n), and -inf in front of it and behind it up to a multiple of G elements (dst starts on
+// Fills a staged row up to whole groups: no mass beside any logit above it, and no infinities in differences.
+constexpr float PAD = -1e30f;
+
+// All threads: src[0, n) to dst[P, P + n), and `pad` in front of it and behind it up to a multiple of G elements (dst starts on
 // 16 bytes, 0 <= P < 8).  16 bytes at a time where src lies P elements behind a 16-byte boundary too; then the first and
 // last elements go one by one, so that nothing outside src is read.  To be followed by cp_async_wait_all and a barrier.
 template <typename T, int G, int THREADS>
-__device__ __forceinline__ void stage_row(T* dst, const T* src, int n, int P) {
+__device__ __forceinline__ void stage_row(T* dst, const T* src, int n, int P, float pad) {
     constexpr int VEC = 16 / sizeof(T);
     const int tid = threadIdx.x, end = P + n;
     const int padded = (end + G - 1) / G * G;
@@ -84,8 +128,8 @@ __device__ __forceinline__ void stage_row(T* dst, const T* src, int n, int P) {
 #pragma unroll 8
         for (int i = tid; i < n; i += THREADS) dst[P + i] = src[i];
     }
-    if (tid < P) dst[tid] = from_f<T>(-INFINITY);
-    if (tid < padded - end) dst[end + tid] = from_f<T>(-INFINITY);
+    if (tid < P) dst[tid] = from_f<T>(pad);
+    if (tid < padded - end) dst[end + tid] = from_f<T>(pad);
 }
 
 // G consecutive elements, aligned to their size.
@@ -165,70 +209,60 @@ __device__ __forceinline__ void put_zeros(T* out, int n) {
 }
 
 // ------------------------------------------------------------------ sums of exponentials
-// 2^{(from - to) c}; zero where nothing was summed.  (to >= from)
+// 2^{(from - to) c}; zero where nothing was summed, 1 where both are infinite.  (to >= from)
 __device__ __forceinline__ float rescale(float from, float to, float c) {
-    return from == -INFINITY ? 0.f : ex2((from - to) * c);
+    return from == -INFINITY ? 0.f : from == to ? 1.f : ex2((from - to) * c);
 }
 
-// A sum of 2^{(x - m) c} with its largest x.
+// A sum z of 2^{(x - m) c}, where m is within reach of its largest x (z neither overflows nor vanishes).
 struct Mass {
-    static constexpr int N = 2;
+    static constexpr int N = 2, SUMS = 1;
     float m, z;
     __device__ __forceinline__ static Mass none() { return {-INFINITY, 0.f}; }
+    __device__ __forceinline__ float* sums() { return &z; }
+    __device__ __forceinline__ void raise(Mass& to) const { to.m = fmaxf(to.m, m); }
+    __device__ __forceinline__ void share() { m = max_of_warp(m); }
+    // against `to`'s reference, which is no less than its own
+    __device__ __forceinline__ Mass against(const Mass& to, float c) const { return {to.m, z * rescale(m, to.m, c)}; }
 };
+
 __device__ __forceinline__ Mass merge(const Mass& x, const Mass& y, float c) {
-    Mass r;
-    r.m = fmaxf(x.m, y.m);
-    r.z = x.z * rescale(x.m, r.m, c) + y.z * rescale(y.m, r.m, c);
-    return r;
+    const Mass to = {fmaxf(x.m, y.m), 0.f};
+    return {to.m, x.against(to, c).z + y.against(to, c).z};
 }
 
 // The masses of two rows s and t over the same entries, and their sums of d = (s - ms) - (t - mt) weighted by each.
-// Against the largest of both, d does not grow with what is common to a row.
+// Against references near the largest of both, d does not grow with what is common to a row.
 struct Pair {
-    static constexpr int N = 6;
-    float ms, zs, as, mt, zt, at;
-    __device__ __forceinline__ static Pair none() { return {-INFINITY, 0.f, 0.f, -INFINITY, 0.f, 0.f}; }
-};
-// x against the maxima ms and mt, which are no less than its own.
-__device__ __forceinline__ Pair rebase(const Pair& x, float ms, float mt, float c) {
-    const float fs = rescale(x.ms, ms, c), ft = rescale(x.mt, mt, c);
-    // (a sum whose row has no mass here is infinite or zero: no shift changes it)
-    const float shift = (x.ms == -INFINITY ? 0.f : x.ms - ms) - (x.mt == -INFINITY ? 0.f : x.mt - mt);
-    // no factor times an infinite sum
-    return {ms, x.zs * fs, fs == 0.f ? 0.f : fs * fmaf(x.zs, shift, x.as), mt, x.zt * ft, ft == 0.f ? 0.f : ft * fmaf(x.zt, shift, x.at)};
-}
-__device__ __forceinline__ Pair merge(const Pair& x, const Pair& y, float c) {
-    const float ms = fmaxf(x.ms, y.ms), mt = fmaxf(x.mt, y.mt);
-    const Pair u = rebase(x, ms, mt, c), v = rebase(y, ms, mt, c);
-    return {ms, u.zs + v.zs, u.as + v.as, mt, u.zt + v.zt, u.at + v.at};
-}
-
-template <typename S>
-__device__ __forceinline__ S merge_warp(S x, float c) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        S y;
-        float* f = reinterpret_cast<float*>(&y);
-        const float* g = reinterpret_cast<const float*>(&x);
-#pragma unroll
-        for (int e = 0; e < S::N; ++e) f[e] = __shfl_xor_sync(0xffffffffu, g[e], o);
-        x = merge(x, y, c);
+    static constexpr int N = 6, SUMS = 4;
+    float ms, mt, zs, zt, as, at;
+    __device__ __forceinline__ static Pair none() { return {-INFINITY, -INFINITY, 0.f, 0.f, 0.f, 0.f}; }
+    __device__ __forceinline__ float* sums() { return &zs; }
+    __device__ __forceinline__ void raise(Pair& to) const { to.ms = fmaxf(to.ms, ms), to.mt = fmaxf(to.mt, mt); }
+    __device__ __forceinline__ void share() { ms = max_of_warp(ms), mt = max_of_warp(mt); }
+    __device__ __forceinline__ Pair against(const Pair& to, float c) const {
+        const float fs = rescale(ms, to.ms, c), ft = rescale(mt, to.mt, c);
+        // (a sum whose row has no mass here is infinite or zero: no shift changes it)
+        const float shift = (ms == -INFINITY ? 0.f : ms - to.ms) - (mt == -INFINITY ? 0.f : mt - to.mt);
+        // no factor of zero times an infinite sum
+        return {to.ms, to.mt, zs * fs, zt * ft, fs == 0.f ? 0.f : fs * fmaf(zs, shift, as), ft == 0.f ? 0.f : ft * fmaf(zt, shift, at)};
     }
-    // lane 0's bits to all: what the lanes hold may differ in the last one
-    float* g = reinterpret_cast<float*>(&x);
+};
+
+// Lane 0's sum in every lane: one order for all.
+__device__ __forceinline__ float sum_of_warp(float v) {
 #pragma unroll
-    for (int e = 0; e < S::N; ++e) g[e] = __shfl_sync(0xffffffffu, g[e], 0);
-    return x;
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
 }
 
-// Places for a CTA's sums of one kind and, in a cluster, the other CTAs'.
+// Places for the sums of a row's warps.
 template <typename S, int THREADS>
 struct Slots {
     S s[ROW_CTAS * THREADS / 32];
 };
-
-// A warp's sums to all CTAs of the row (of which there are several: they have waited for one another's start), or to its own.
+// A warp's sums (the same in all lanes) to all CTAs of the row (of which there are several: they have waited for one
+// another's start), or to its own.
 template <typename S, int THREADS>
 __device__ __forceinline__ void post(const S& x, Slots<S, THREADS>& slots, int ctas) {
     constexpr int WARPS = THREADS / 32;
@@ -255,9 +289,21 @@ __device__ __forceinline__ void posted(int ctas) {
 // The row's sums from its warps', the same bits in every thread.
 template <typename S, int THREADS>
 __device__ __forceinline__ S collect(const Slots<S, THREADS>& slots, int ctas, float c) {
-    S r = S::none();
-    for (int j = threadIdx.x & 31; j < THREADS / 32 * ctas; j += 32) r = merge(r, slots.s[j], c);
-    return merge_warp(r, c);
+    const int lane = threadIdx.x & 31, count = THREADS / 32 * ctas;
+    S top = S::none();
+    for (int j = lane; j < count; j += 32) slots.s[j].raise(top);
+    top.share();
+    S r = top;
+#pragma unroll
+    for (int e = 0; e < S::SUMS; ++e) r.sums()[e] = 0.f;
+    for (int j = lane; j < count; j += 32) {
+        S x = slots.s[j].against(top, c);
+#pragma unroll
+        for (int e = 0; e < S::SUMS; ++e) r.sums()[e] += x.sums()[e];
+    }
+#pragma unroll
+    for (int e = 0; e < S::SUMS; ++e) r.sums()[e] = sum_of_warp(r.sums()[e]);
+    return r;
 }
 
 // ------------------------------------------------------------------ launches

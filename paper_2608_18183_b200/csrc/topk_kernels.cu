@@ -79,11 +79,12 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
 }
 
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a, int cap) {
     constexpr int G = 16 / sizeof(T), WARPS = THREADS / 32, SETS = 4;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ Slots<Mass, THREADS> slots, slots_all;
+    __shared__ Mass slots[ROW_CTAS], slots_all[WARPS];  // the slices' rests; the warps' of what no list keeps
     __shared__ uint32_t hist[BINS], red[2][WARPS];
+    __shared__ float sums[WARPS];
     __shared__ int found;
     pdl_wait();
     pdl_trigger();
@@ -102,7 +103,7 @@ __global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
     T* xs = (T*)smem;
     unsigned long long* cand = (unsigned long long*)(smem + (a.slice + 16) * sizeof(T));
     unsigned long long* lists = cand + cap;  // [ctas][k], several CTAs only
-    stage_row<T, G, THREADS>(xs, src, n, P);
+    stage_row<T, G, THREADS>(xs, src, n, P, -INFINITY);
     if (tid == 0) found = 0;
     cp_async_wait_all();
     __syncthreads();
@@ -162,30 +163,39 @@ __global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
                     if (i < sets) f(key[i]);
             });
     }
-    // ---- candidates, and the mass of all others
+    // ---- candidates, and the mass of all others against the bound
     const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
-    Mass rest;
+    const f32x2 c2 = both(c);
+    float z, t;
     bool tied = false;  // too many entries equal the k-th: only those beyond it are candidates yet
-    int above = 0;      // (if so) the entries that reach it
+    int reach = 0;      // (if so) the entries that reach it
     while (true) {
-        const float t = value_of(thr);
-        float z = 0.f;
+        t = value_of(thr);
+        const f32x2 o = both(-t);
+        f32x2 z2 = both(0.f);
         for (int j = tid; j < groups; j += THREADS) {
             float x[G];
             get<G>(xs + j * G, x);
+            float most = x[0];
 #pragma unroll
-            for (int i = 0; i < G; ++i) {
-                if (x[i] >= t) {
-                    if (!tied || x[i] > t) {
-                        const int p = atomicAdd(&found, 1);
-                        if (p < cap) cand[p] = rank_key(x[i], v0 + j * G + i - P);
+            for (int i = 1; i < G; ++i) most = fmaxf(most, x[i]);
+            if (most >= t) {
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    if (x[i] >= t) {
+                        if (!tied || x[i] > t) {
+                            const int p = atomicAdd(&found, 1);
+                            if (p < cap) cand[p] = rank_key(x[i], v0 + j * G + i - P);
+                        }
+                        x[i] = -INFINITY;
                     }
-                } else {
-                    z += x[i] > -INFINITY ? ex2((x[i] - t) * c) : 0.f;  // (t may be infinite; NaN counts as -inf)
-                }
+            }
+            if (a.rest) {
+#pragma unroll
+                for (int i = 0; i < G; i += 2) z2 = add2(z2, ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)));
             }
         }
-        rest = {t, z};
+        z = sum2(z2);
         __syncthreads();
         if (found <= cap) break;
         // the entries that reach the bound, narrowed until they fit; the k-th largest itself if they never do
@@ -201,7 +211,7 @@ __global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
             }
         });
         // (where more than cap entries reach it still, it is the k-th largest: fewer than k lie above)
-        int reach = 0;
+        reach = 0;
         const float u = value_of(thr);
         for (int j = tid; j < groups; j += THREADS) {
             float x[G];
@@ -215,31 +225,9 @@ __global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
         reach = __reduce_add_sync(0xffffffffu, lane < WARPS ? red[0][lane % WARPS] : 0);
         tied = reach > cap;
         __syncthreads();
-        above = reach;
-    }
-    if (thr != LOWEST_KEY && rest.z < 1e-25f) {  // far below the bound, where digits or all were lost: against the largest of them
-        const float t = value_of(thr);
-        float m = -INFINITY, z = 0.f;
-        for (int j = tid; j < groups; j += THREADS) {
-            float x[G];
-            get<G>(xs + j * G, x);
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-                if (x[i] < t) m = fmaxf(m, x[i]);
-        }
-        for (int j = tid; j < groups && m > -INFINITY; j += THREADS) {
-            float x[G];
-            get<G>(xs + j * G, x);
-#pragma unroll
-            for (int i = 0; i < G; ++i)
-                if (x[i] < t) z += ex2((x[i] - m) * c);
-        }
-        rest = {m, z};
     }
     int count = found;
     if (tied) {  // the first of the tied entries, by index
-        const float t = value_of(thr);
-        const int beyond = count;
         for (int e0 = 0; e0 < P + n && count < k; e0 += THREADS) {
             const int e = e0 + tid;
             const bool is = e < P + n && to_f<T>(xs[e]) == t;
@@ -255,16 +243,11 @@ __global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
             count = min(k, count + all);
             __syncthreads();
         }
-        // those that were not taken
-        const int left = (above - beyond) - (count - beyond);
-        if (tid == 0 && left > 0) rest = merge(rest, {t, (float)left}, c);
+        if (tid == 0) z += (float)(reach - count);  // those that were not taken
     }
     __syncthreads();
 
     // ---- order
-    const auto leave = [&](unsigned long long key) {  // a candidate behind the k-th
-        rest = merge(rest, {value_of((uint32_t)(key >> 32)), 1.f}, c);
-    };
     float* values = a.values + to * k;
     int32_t* indices = a.indices + to * k;
     const auto place = [&](int r, unsigned long long key) {
@@ -307,16 +290,58 @@ __global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
             }
         __syncthreads();
     }
+    // (where every entry is a candidate, none was summed yet, and the bound is no entry)
+    if (thr == LOWEST_KEY && count > k) t = value_of((uint32_t)(sorted[k - 1] >> 32));
     for (int i = tid; i < max(count, k); i += THREADS)
         if (i < k)
             place(i, i < count ? sorted[i] : 0);
-        else
-            leave(sorted[i]);
-    rest = merge_warp(rest, c);
-    post(rest, slots, a.ctas);
-    posted(a.ctas);
-    rest = collect(slots, a.ctas, c);
+        else  // a candidate behind the k-th
+            z += ex2((value_of((uint32_t)(sorted[i] >> 32)) - t) * c);
+
+    // ---- the rest
+    Mass rest = {t, 0.f};
+    if (a.rest) {
+        z = sum_of_warp(z);
+        if (lane == 0) sums[wid] = z;
+        __syncthreads();
+        rest.z = sum_of_warp(lane < WARPS ? sums[lane % WARPS] : 0.f);
+        // NaN in the row, or all of the rest far off the bound: again, against its largest and passing NaN over
+        if (!(rest.z > 1e-20f && rest.z < 1e20f)) {
+            const auto each = [&](auto&& f) {
+                for (int j = tid; j < groups; j += THREADS) {
+                    float x[G];
+                    get<G>(xs + j * G, x);
+#pragma unroll
+                    for (int i = 0; i < G; ++i)
+                        if (x[i] < value_of(thr)) f(x[i], 1.f);
+                }
+                for (int i = k + tid; i < count; i += THREADS) f(value_of((uint32_t)(sorted[i] >> 32)), 1.f);
+                if (tied && tid == 0 && reach > count) f(t, (float)(reach - count));
+            };
+            float m = -INFINITY;
+            each([&](float x, float) { m = fmaxf(m, x); });
+            m = max_of_warp(m);
+            __syncthreads();
+            if (lane == 0) sums[wid] = m;
+            __syncthreads();
+            m = max_of_warp(sums[lane % WARPS]);
+            z = 0.f;
+            const float o = m == -INFINITY ? 0.f : m;
+            each([&](float x, float times) { z += x == m ? times : times * ex2((x - o) * c); });
+            z = sum_of_warp(z);
+            __syncthreads();
+            if (lane == 0) sums[wid] = z;
+            __syncthreads();
+            rest = {m, m == -INFINITY ? 0.f : sum_of_warp(lane < WARPS ? sums[lane % WARPS] : 0.f)};
+        }
+    }
     if (a.ctas > 1) {
+        if (tid == 0) {
+            const uint32_t place = remote_smem(&slots[rank], 0);
+            remote_store(place, rest.m);
+            remote_store(place + 4, rest.z);
+        }
+        posted(a.ctas);
         if (rank) return;
         // the lists of all slices: an entry's place is its own list's and, for each other, the entries that come first
         Mass mine = Mass::none();
@@ -348,10 +373,16 @@ __global__ void __launch_bounds__(THREADS) k_topk(TopkArgs a, int cap) {
         }
         valid = __reduce_add_sync(0xffffffffu, valid);
         if (lane == 0) red[0][wid] = valid;
-        if (tid == 0) mine = merge(mine, rest, c);
-        post(merge_warp(mine, c), slots_all, 1);
-        posted(1);
-        rest = collect(slots_all, 1, c);
+        if (tid < a.ctas) mine = merge(mine, slots[tid], c);
+        Mass all = mine;
+        all.share();
+        all.z = sum_of_warp(mine.against(all, c).z);
+        if (lane == 0) slots_all[wid] = all;
+        __syncthreads();
+        mine = lane < WARPS ? slots_all[lane] : Mass::none();
+        rest = mine;
+        rest.share();
+        rest.z = sum_of_warp(mine.against(rest, c).z);
         valid = __reduce_add_sync(0xffffffffu, lane < WARPS ? red[0][lane % WARPS] : 0);
         for (int i = valid + tid; i < k; i += THREADS) {
             values[i] = -INFINITY;
