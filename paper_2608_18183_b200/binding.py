@@ -168,70 +168,75 @@ def hbsjd_verify_static(stream, desc, logits, q_prev, p_out, cursor, seq, delta,
 # Tensors lie on one GPU, which need not be the current one.  A call goes to `stream`, or to the current stream of the tensors'
 # device; inputs made on another stream have to be ordered before it by the caller, and nothing waits for the result.
 
-class _Rows:
-    """One call: checks its tensors as they are passed in, then makes it on their device."""
+_torch = None
+_types = {}
 
-    def __init__(self, what, logits, stream):
+
+def _refuse(what, why):
+    raise HbsjdError(-1, what, why)
+
+
+def _rows(what, name, x, device=None, dtype=None, shape=None, written=False):
+    """(pointer, row stride, type) of a matrix of logits or of another element type whose rows' elements are neighbours."""
+    global _torch, _types
+    if _torch is None:
         import torch
-        self.torch, self.what, self.stream = torch, what, stream
-        self.types = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
-        self.device = None
-        self.kept = []
-        self.rows, self.V = 0, 0
-        self.matrix(logits, "logits")
-        self.rows, self.V = logits.shape
-        if self.stream is not None and self.stream.device != self.device:
-            self.refuse(f"stream of {self.stream.device}, tensors on {self.device}")
+        _torch, _types = torch, {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+    if not isinstance(x, _torch.Tensor) or not x.is_cuda:
+        _refuse(what, f"{name} is not a tensor on a GPU")
+    if device is not None and x.device != device:
+        _refuse(what, f"{name} lies on {x.device}, not on {device}")
+    own = x.dtype
+    if own not in _types if dtype is None else own != dtype:
+        _refuse(what, f"{name} has type {own}")
+    size = x.shape
+    if len(size) != 2 or shape is not None and size != shape:
+        _refuse(what, f"{name} has shape {tuple(size)}" + (f", not {tuple(shape)}" if shape is not None else ""))
+    ld, step = x.stride()
+    if step != 1 and size[1] > 1:
+        _refuse(what, f"{name}: the elements of a row are not neighbours")
+    if size[0] <= 1:
+        ld = size[1]
+    if written and ld < size[1]:
+        _refuse(what, f"{name}: rows overlap")
+    return x.data_ptr(), ld, _types.get(own)
 
-    def refuse(self, why):
-        raise HbsjdError(-1, self.what, why)
 
-    def _placed(self, x, name):
-        if not isinstance(x, self.torch.Tensor) or not x.is_cuda:
-            self.refuse(f"{name} is not a tensor on a GPU")
-        if self.device is None:
-            self.device = x.device
-        if x.device != self.device:
-            self.refuse(f"{name} lies on {x.device}, not on {self.device}")
-        self.kept.append(x)
+def _vector(what, name, x, device, dtype, n):
+    """Pointer of a contiguous vector, or None."""
+    if x is None:
+        return None
+    if not isinstance(x, _torch.Tensor) or x.device != device or x.dtype != dtype or x.shape != (n,) or (
+            n > 1 and x.stride(0) != 1):
+        _refuse(what, f"{name} has to be contiguous, of type {dtype} and shape ({n},), on {device}")
+    return x.data_ptr()
 
-    def matrix(self, x, name, dtype=None, shape=None, written=False):
-        """(pointer, row stride, type) of rows whose elements are neighbours."""
-        self._placed(x, name)
-        if dtype is None and x.dtype not in self.types or dtype is not None and x.dtype != dtype:
-            self.refuse(f"{name} has type {x.dtype}")
-        if x.dim() != 2 or shape is not None and tuple(x.shape) != tuple(shape):
-            self.refuse(f"{name} has shape {tuple(x.shape)}" + (f", not {tuple(shape)}" if shape is not None else ""))
-        if x.shape[1] > 1 and x.stride(1) != 1:
-            self.refuse(f"{name}: the elements of a row are not neighbours")
-        ld = x.stride(0) if x.shape[0] > 1 else x.shape[1]
-        if written and ld < x.shape[1]:
-            self.refuse(f"{name}: rows overlap")
-        return x.data_ptr(), ld, self.types.get(x.dtype)
 
-    def vector(self, x, name, dtype, n):
-        if x is None:
-            return None
-        self._placed(x, name)
-        if x.dtype != dtype or tuple(x.shape) != (n,) or not x.is_contiguous():
-            self.refuse(f"{name} has to be contiguous, of type {dtype} and shape ({n},)")
-        return x.data_ptr()
+def _on(what, stream, device):
+    """Runs the rest of a call on the tensors' device, with `stream` current if one is given."""
+    if stream is None:
+        return _torch.cuda.device(device)
+    if stream.device != device:
+        _refuse(what, f"stream of {stream.device}, tensors on {device}")
+    return _torch.cuda.stream(stream)
 
-    def new(self, shape, dtype):
-        with self.torch.cuda.device(self.device), self.torch.cuda.stream(self.stream):
-            return self.torch.empty(shape, dtype=dtype, device=self.device)
 
-    def call(self, entry, desc, *pointers):
-        torch = self.torch
-        with torch.cuda.device(self.device):
-            stream = self.stream if self.stream is not None else torch.cuda.current_stream()
-            rc = entry(C.c_void_p(stream.cuda_stream), C.byref(desc), *pointers)
-        if rc != 0:
-            raise HbsjdError(rc, self.what, load().hbsjd_last_error(None).decode())
-        if self.stream is not None:
-            # memory that its owner gives back is not to be used again before this call has run
-            for x in self.kept:
-                x.record_stream(self.stream)
+def _call(what, entry, device, desc, *pointers):
+    rc = entry(_torch._C._cuda_getCurrentRawStream(device.index), desc, *pointers)
+    if rc != 0:
+        raise HbsjdError(rc, what, load().hbsjd_last_error(None).decode())
+
+
+def _elsewhere(f, what, logits, stream, args, kw):
+    """f again, where its tensors' device and the stream it is to use are the current ones."""
+    with _on(what, stream, logits.device):
+        out = f(*args, **kw)
+    if stream is not None:
+        # memory that its owner gives back is not to be used again before this call has run
+        for x in (*args, *kw.values()):
+            if isinstance(x, _torch.Tensor):
+                x.record_stream(stream)
+    return out
 
 
 def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=None, mask_row=None, history=None,
@@ -240,66 +245,86 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
     """Guidance, penalties, bias and masks on [rows, V] logits of fp32 or bf16 -> out, a new tensor or the given one (which may
     be `logits`).  mask: int32 or uint32 words [masks, words], history: int32 [sequences, tokens], row numbers and
     lengths int32 [rows], bias fp32 [V]."""
-    c = _Rows("hbsjd_adjust_logits", logits, stream)
-    torch, rows, V = c.torch, c.rows, c.V
-    x, ld, dtype = c.matrix(logits, "logits")
+    what = "hbsjd_adjust_logits"
+    x, ld, dtype = _rows(what, "logits", logits)
+    device = logits.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_adjust_logits, what, logits, stream,
+                          (logits, logits_u, cfg_scale, bias, mask, mask_row, history, history_row, history_len, repetition,
+                           frequency, presence, out), {})
+    shape, i32 = logits.shape, _torch.int32
+    rows, V = shape
     u, ld_u = None, 0
     if logits_u is not None:
-        u, ld_u, _ = c.matrix(logits_u, "logits_u", logits.dtype, (rows, V))
-    words, ld_mask = None, 0
+        u, ld_u, _ = _rows(what, "logits_u", logits_u, device, logits.dtype, shape)
+    words, ld_mask, masks = None, 0, 0
     if mask is not None:
-        words, ld_mask, _ = c.matrix(mask, "mask", torch.uint32 if getattr(mask, "dtype", None) == torch.uint32
-                                     else torch.int32)
+        words, ld_mask, _ = _rows(what, "mask", mask, device, i32 if getattr(mask, "dtype", None) == i32 else _torch.uint32)
+        masks = mask.shape[0]
         if mask.shape[1] < (V + 31) // 32:
-            c.refuse(f"mask has {mask.shape[1]} words for {V} entries")
-        if mask.shape[0] > 1 and ld_mask < mask.shape[1]:
-            c.refuse("mask: rows overlap")
-        ld_mask = max(ld_mask, mask.shape[1])
-    tok, ld_history = None, 0
-    if history is not None and history.shape[-1] > 0:
-        tok, ld_history, _ = c.matrix(history, "history", torch.int32)
-        if history.shape[0] > 1 and ld_history < history.shape[1]:
-            c.refuse("history: rows overlap")
+            _refuse(what, f"mask has {mask.shape[1]} words for {V} entries")
+        if masks == 0:
+            words = None
+        elif ld_mask < mask.shape[1]:
+            _refuse(what, "mask: rows overlap")
+    tok, ld_history, sequences, cap = None, 0, 0, 0
+    if history is not None:
+        tok, ld_history, _ = _rows(what, "history", history, device, i32, written=True)
+        sequences, cap = history.shape
+        if not sequences or not cap:
+            tok = None
     if out is None:
-        out = c.new((rows, V), logits.dtype)
-    o, ld_out, _ = c.matrix(out, "out", logits.dtype, (rows, V), written=True)
-    d = hbsjd_adjust_desc(rows, V, dtype, 0 if words is None else mask.shape[0], 0 if tok is None else history.shape[0],
-                          0 if tok is None else history.shape[1], ld, ld_u, ld_out, ld_mask, ld_history, cfg_scale,
-                          repetition, frequency, presence)
-    c.call(load().hbsjd_adjust_logits, d, x, u, c.vector(bias, "bias", torch.float32, V), words,
-           c.vector(mask_row, "mask_row", torch.int32, rows), tok, c.vector(history_row, "history_row", torch.int32, rows),
-           c.vector(history_len, "history_len", torch.int32, rows), o)
+        out = logits.new_empty(shape)
+    o, ld_out, _ = _rows(what, "out", out, device, logits.dtype, shape, written=True)
+    if rows == 0:
+        return out
+    d = hbsjd_adjust_desc(rows, V, dtype, masks, sequences, cap, ld, ld_u, ld_out, ld_mask, ld_history, cfg_scale, repetition,
+                          frequency, presence)
+    _call(what, load().hbsjd_adjust_logits, device, d, x, u, _vector(what, "bias", bias, device, _torch.float32, V), words,
+          _vector(what, "mask_row", mask_row, device, i32, rows), tok,
+          _vector(what, "history_row", history_row, device, i32, rows),
+          _vector(what, "history_len", history_len, device, i32, rows), o)
     return out
 
 
 def hbsjd_topk_logits(logits, k, temperature=1.0, want_rest=True, stream=None):
     """The k largest logits of each row of [rows, V]: (values fp32 [rows, k], indices int32 [rows, k], rest fp32 [rows] or
     None)."""
-    c = _Rows("hbsjd_topk_logits", logits, stream)
-    torch = c.torch
-    x, ld, dtype = c.matrix(logits, "logits")
-    if not 1 <= k <= min(c.V, 1024):
-        c.refuse(f"k = {k} is out of range")
-    values, indices = c.new((c.rows, k), torch.float32), c.new((c.rows, k), torch.int32)
-    rest = c.new((c.rows,), torch.float32) if want_rest else None
-    c.call(load().hbsjd_topk_logits, hbsjd_topk_desc(c.rows, c.V, dtype, k, ld, temperature, 0), x, values.data_ptr(),
-           indices.data_ptr(), None if rest is None else rest.data_ptr())
+    what = "hbsjd_topk_logits"
+    x, ld, dtype = _rows(what, "logits", logits)
+    device = logits.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_topk_logits, what, logits, stream, (logits, k, temperature, want_rest), {})
+    rows, V = logits.shape
+    if not 1 <= k <= min(V, 1024):
+        _refuse(what, f"k = {k} is out of range")
+    values = logits.new_empty((rows, k), dtype=_torch.float32)
+    indices = logits.new_empty((rows, k), dtype=_torch.int32)
+    rest = logits.new_empty((rows,), dtype=_torch.float32) if want_rest else None
+    if rows:
+        _call(what, load().hbsjd_topk_logits, device, hbsjd_topk_desc(rows, V, dtype, k, ld, temperature, 0), x,
+              values.data_ptr(), indices.data_ptr(), rest.data_ptr() if want_rest else None)
     return values, indices, rest
 
 
-def _distill(c, logits_s, weight, temperature, forward, reverse, want_grad, grad, k=0, dtype_t=0, ld_t=0):
-    """Descriptor, pointers and outputs that both forms of the divergence share."""
-    torch = c.torch
-    s, ld_s, dtype_s = c.matrix(logits_s, "logits_s")
-    if want_grad and grad is None:
-        grad = c.new((c.rows, c.V), logits_s.dtype)
-    g, ld_g = None, 0
+def _distill(what, entry, logits_s, s, ld_s, dtype_s, teacher, dtype_t, ld_t, k, weight, temperature, forward, reverse,
+             want_grad, grad):
+    """What both forms of the divergence share: the gradient and the loss, and the call."""
+    shape, device = logits_s.shape, logits_s.device
+    rows, V = shape
     if grad is not None:
-        g, ld_g, _ = c.matrix(grad, "grad", logits_s.dtype, (c.rows, c.V), written=True)
-    w = c.vector(weight, "weight", torch.float32, c.rows)
-    loss = c.new((c.rows,), torch.float32)
-    d = hbsjd_distill_desc(c.rows, c.V, dtype_s, dtype_t, k, 0, ld_s, ld_t, ld_g, temperature, forward, reverse, 0)
-    return d, s, w, loss, grad, g
+        g, ld_g, _ = _rows(what, "grad", grad, device, logits_s.dtype, shape, written=True)
+    elif want_grad:
+        grad = logits_s.new_empty(shape)
+        g, ld_g = grad.data_ptr(), V
+    else:
+        g, ld_g = None, 0
+    w = _vector(what, "weight", weight, device, _torch.float32, rows)
+    loss = logits_s.new_empty((rows,), dtype=_torch.float32)
+    if rows:
+        d = hbsjd_distill_desc(rows, V, dtype_s, dtype_t, k, 0, ld_s, ld_t, ld_g, temperature, forward, reverse, 0)
+        _call(what, entry, device, d, s, *teacher, w, loss.data_ptr(), g)
+    return loss, grad
 
 
 def hbsjd_distill(logits_s, logits_t, weight=None, temperature=1.0, forward=0.5, reverse=0.5, want_grad=True, grad=None,
@@ -307,31 +332,35 @@ def hbsjd_distill(logits_s, logits_t, weight=None, temperature=1.0, forward=0.5,
     """forward KL(p || q) + reverse KL(q || p) of each row of the student's [rows, V] logits (q) against the teacher's (p), and
     weight times its gradient in logits_s: (loss fp32 [rows], grad like logits_s or None).  The defaults are Eq. 3.
     grad: a tensor for the gradient, which may be logits_s.  In a training step: logits_s.backward(grad)."""
-    c = _Rows("hbsjd_distill", logits_s, stream)
-    t, ld_t, dtype_t = c.matrix(logits_t, "logits_t", None, (c.rows, c.V))
-    d, s, w, loss, grad, g = _distill(c, logits_s, weight, temperature, forward, reverse, want_grad, grad,
-                                      dtype_t=dtype_t, ld_t=ld_t)
-    c.call(load().hbsjd_distill, d, s, t, w, loss.data_ptr(), g)
-    return loss, grad
+    what = "hbsjd_distill"
+    s, ld_s, dtype_s = _rows(what, "logits_s", logits_s)
+    device = logits_s.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_distill, what, logits_s, stream,
+                          (logits_s, logits_t, weight, temperature, forward, reverse, want_grad, grad), {})
+    t, ld_t, dtype_t = _rows(what, "logits_t", logits_t, device, None, logits_s.shape)
+    return _distill(what, load().hbsjd_distill, logits_s, s, ld_s, dtype_s, (t,), dtype_t, ld_t, 0, weight, temperature,
+                    forward, reverse, want_grad, grad)
 
 
 def hbsjd_distill_topk(logits_s, values, indices, rest=None, weight=None, temperature=1.0, forward=1.0, reverse=0.0,
                        want_grad=True, grad=None, stream=None):
     """hbsjd_distill against a teacher that is given by its largest logits: values fp32 and indices int32 [rows, k], rest fp32
     [rows] (the tokens that are not listed as one outcome) or None (renormalised over the list)."""
-    c = _Rows("hbsjd_distill_topk", logits_s, stream)
-    torch = c.torch
-    if not isinstance(values, torch.Tensor) or values.dim() != 2:
-        c.refuse("values is not a matrix")
-    k = values.shape[1]
-    for x, name, dtype in ((values, "values", torch.float32), (indices, "indices", torch.int32)):
-        c.matrix(x, name, dtype, (c.rows, k))
-        if not x.is_contiguous():
-            c.refuse(f"{name} is not contiguous")
-    r = c.vector(rest, "rest", torch.float32, c.rows)
-    d, s, w, loss, grad, g = _distill(c, logits_s, weight, temperature, forward, reverse, want_grad, grad, k=k)
-    c.call(load().hbsjd_distill_topk, d, s, values.data_ptr(), indices.data_ptr(), r, w, loss.data_ptr(), g)
-    return loss, grad
+    what = "hbsjd_distill_topk"
+    s, ld_s, dtype_s = _rows(what, "logits_s", logits_s)
+    device = logits_s.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_distill_topk, what, logits_s, stream,
+                          (logits_s, values, indices, rest, weight, temperature, forward, reverse, want_grad, grad), {})
+    v, ld_v, _ = _rows(what, "values", values, device, _torch.float32)
+    rows, k = values.shape
+    i, ld_i, _ = _rows(what, "indices", indices, device, _torch.int32, values.shape)
+    if rows != logits_s.shape[0] or ld_v != k or ld_i != k:
+        _refuse(what, f"values and indices have to be contiguous, with {logits_s.shape[0]} rows")
+    r = _vector(what, "rest", rest, device, _torch.float32, rows)
+    return _distill(what, load().hbsjd_distill_topk, logits_s, s, ld_s, dtype_s, (v, i, r), 0, 0, k, weight, temperature,
+                    forward, reverse, want_grad, grad)
 
 
 class Context:
