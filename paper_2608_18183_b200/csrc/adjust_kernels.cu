@@ -30,12 +30,13 @@ __device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t*
             any |= (q.x | q.y | q.z | q.w) != 0;
         }
         if (any) {
+            // (without a branch: some lane of a warp has such a token nearly always)
+            const float inv = 1.f / a.repetition;
 #pragma unroll
-            for (int i = 0; i < G; ++i)
-                if (n[i]) {
-                    x[i] = x[i] > 0.f ? x[i] / a.repetition : x[i] * a.repetition;
-                    x[i] -= fmaf((float)n[i], a.frequency, a.presence);
-                }
+            for (int i = 0; i < G; ++i) {
+                const float y = x[i] * (x[i] > 0.f ? inv : a.repetition) - fmaf((float)n[i], a.frequency, a.presence);
+                x[i] = n[i] ? y : x[i];
+            }
         }
     }
     if (a.bias) {
@@ -135,7 +136,7 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
             }
         }
         apply_rules<G>(a, bits, counts, y, v0 + e, P + e);
-        put_at<T, G>(out, e, n, y);
+        put_at<T, G>(out, e, 0, n, y);
     }
 }
 

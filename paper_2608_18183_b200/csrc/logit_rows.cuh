@@ -13,7 +13,7 @@ namespace hbsjd {
 constexpr int MAX_LOGIT_V = 131072;    // entries of a row: what eight CTAs hold of two fp32 rows
 constexpr int MAX_LISTED = 1024;       // entries of a top-K list
 constexpr int ROW_CTAS = 8;            // CTAs of a row, at most (the portable cluster size)
-constexpr int ROW_SMEM = 200 * 1024;   // dynamic shared memory that a CTA may ask for
+constexpr int ROW_SMEM = 216 * 1024;   // dynamic shared memory that a CTA may ask for
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
@@ -21,6 +21,13 @@ constexpr float LN2 = 0.6931471805599453f;
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// log2(x) within 2^-22 (absolute for x in (0.5, 2), else relative): no worse than the sums it is taken of.
+__device__ __forceinline__ float lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 
@@ -94,6 +101,14 @@ __device__ __forceinline__ void cp_async4(void* dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All of this thread's groups but the last `pending` (0 or 1) have arrived.
+__device__ __forceinline__ void cp_async_wait(int pending) {
+    if (pending)
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
 
 // Place of a row's first element behind a 16-byte boundary, in elements.
 template <typename T>
@@ -104,30 +119,43 @@ __device__ __forceinline__ int phase_of(const T* p) {
 // Fills a staged row up to whole groups: no mass beside any logit above it, and no infinities in differences.
 constexpr float PAD = -1e30f;
 
-// All threads: src[0, n) to dst[P, P + n), and `pad` in front of it and behind it up to a multiple of G elements (dst starts on
-// 16 bytes, 0 <= P < 8).  16 bytes at a time where src lies P elements behind a 16-byte boundary too; then the first and
-// last elements go one by one, so that nothing outside src is read.  To be followed by cp_async_wait_all and a barrier.
-template <typename T, int G, int THREADS>
-__device__ __forceinline__ void stage_row(T* dst, const T* src, int n, int P, float pad) {
-    constexpr int VEC = 16 / sizeof(T);
+// All threads: begins the copy of src[0, n) to dst[P, P + n) (dst starts on 16 bytes, 0 <= P < 8).  16 bytes at a time
+// where src lies P elements behind a 16-byte boundary too, 4 where it lies so behind a 4-byte boundary, else one by one.  Of bf16, the 4
+// bytes that hold src's first or last element may hold one of a neighbour: it is copied too.  Then
+// cp_async_wait_all, a barrier, end_row and a barrier.
+template <typename T, int THREADS>
+__device__ __forceinline__ void stage_row(T* dst, const T* src, int n, int P) {
+    constexpr int VEC = 16 / sizeof(T), W = 4 / sizeof(T);
     const int tid = threadIdx.x, end = P + n;
-    const int padded = (end + G - 1) / G * G;
+    const T* base = src - P;
+    if (n <= 0) return;
     if (phase_of(src) == P % VEC) {
         const int first = (P + VEC - 1) / VEC, last = end / VEC;  // whole vectors
-        const T* base = src - P;
 #pragma unroll 4
         for (int j = first + tid; j < last; j += THREADS) cp_async16(dst + j * VEC, base + j * VEC);
-        // fewer than VEC elements in front, fewer than VEC behind
-        const int head_end = min(first * VEC, end), tail = max(last * VEC, head_end);
-        if (tid < head_end - P) dst[P + tid] = src[tid];
-        if (tid < end - tail) dst[tail + tid] = src[tail - P + tid];
-    } else if (sizeof(T) == 4) {
+        // words of the less than VEC elements in front, and of those behind
+        const int head_end = min(first * VEC, end), tail = max(last * VEC, head_end), w = P / W + tid;
+        if (w * W < head_end) cp_async4(dst + w * W, base + w * W);
+        if (tid >= 32 && tail + (tid - 32) * W < end) cp_async4(dst + tail + (tid - 32) * W, base + tail + (tid - 32) * W);
+    } else if ((phase_of(src) - P) % W == 0) {
 #pragma unroll 8
-        for (int i = tid; i < n; i += THREADS) cp_async4(dst + P + i, src + i);
+        for (int w = P / W + tid; w * W < end; w += THREADS) cp_async4(dst + w * W, base + w * W);
     } else {
-#pragma unroll 8
-        for (int i = tid; i < n; i += THREADS) dst[P + i] = src[i];
+        for (int i = tid; i < n; i += THREADS * 8) {
+            T x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i + u * THREADS < n) x[u] = src[i + u * THREADS];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i + u * THREADS < n) dst[P + i + u * THREADS] = x[u];
+        }
     }
+}
+// `pad` in front of a staged row and behind it up to a multiple of G elements.
+template <typename T, int G>
+__device__ __forceinline__ void end_row(T* dst, int n, int P, float pad) {
+    const int tid = threadIdx.x, end = P + n, padded = (end + G - 1) / G * G;
     if (tid < P) dst[tid] = from_f<T>(pad);
     if (tid < padded - end) dst[end + tid] = from_f<T>(pad);
 }
@@ -177,35 +205,103 @@ __device__ __forceinline__ void put(bf16* p, const float (&x)[G]) {
         __stcs(reinterpret_cast<uint4*>(p),
                make_uint4(pack(x[0], x[1]), pack(x[2], x[3]), pack(x[4], x[5]), pack(x[6], x[7])));
 }
-// G elements of a staged row from its element i on (element 0 lies at p[P]), those outside [0, n) -inf or anything.  wide: i + P
-// is a multiple of G.
+// The elements of [i, i + G) that lie in [lo, hi) to out (out + i lies on a multiple of G elements).
 template <typename T, int G>
-__device__ __forceinline__ void get_at(const T* p, int P, int i, int n, bool wide, float (&x)[G]) {
-    if (wide) {
-        get<G>(p + P + i, x);
-    } else {
-#pragma unroll
-        for (int e = 0; e < G; ++e) x[e] = i + e >= 0 && i + e < n ? to_f<T>(p[P + i + e]) : -INFINITY;
-    }
-}
-// The elements of [i, i + G) that lie in [0, n) to out (out + i lies on a multiple of G elements).
-template <typename T, int G>
-__device__ __forceinline__ void put_at(T* out, int i, int n, const float (&x)[G]) {
-    if (i >= 0 && i + G <= n) {
+__device__ __forceinline__ void put_at(T* out, int i, int lo, int hi, const float (&x)[G]) {
+    if (i >= lo && i + G <= hi) {
         put<G>(out + i, x);
     } else {
 #pragma unroll
         for (int e = 0; e < G; ++e)
-            if (i + e >= 0 && i + e < n) out[i + e] = from_f<T>(x[e]);
+            if (i + e >= lo && i + e < hi) out[i + e] = from_f<T>(x[e]);
     }
 }
-// out[0, n) = 0, wide where out's alignment allows it.
-template <typename T, int THREADS>
-__device__ __forceinline__ void put_zeros(T* out, int n) {
+
+// ------------------------------------------------------------------ a warp's part of a row
+// A slice of n elements, the first of them P elements behind a 16-byte boundary in shared memory, as groups of G; a warp has the
+// groups [j0, j1) to itself.  It stages them, sums over them and writes their gradient without waiting for other warps.
+template <int G, int WARPS>
+struct Part {
+    int P, n, j0, j1;
+    __device__ __forceinline__ Part(int P, int n) : P(P), n(n) {
+        const int groups = (P + n + G - 1) / G, each = ((groups + WARPS - 1) / WARPS + 1) / 2 * 2;  // (even: 16 bytes of bf16)
+        j0 = min((int)(threadIdx.x >> 5) * each, groups);
+        j1 = min(j0 + each, groups);
+    }
+    // groups [inner(), outer()) are the row's in whole
+    __device__ __forceinline__ int inner() const { return j0 * G >= P ? j0 : min((P + G - 1) / G, j1); }
+    __device__ __forceinline__ int outer() const { return max(min(j1, (P + n) / G), inner()); }
+    // staged elements [first(), last()) are the row's, in it from element first() - P on
+    __device__ __forceinline__ int first() const { return max(j0 * G, P); }
+    __device__ __forceinline__ int last() const { return min(j1 * G, P + n); }
+};
+
+// The words of the less than 16 bytes in front of the part's whole vectors, and of those behind.
+template <typename T, int G, int WARPS>
+__device__ __forceinline__ void stage_ends(T* dst, const T* src, const Part<G, WARPS>& p) {
+    constexpr int VEC = 16 / sizeof(T), W = 4 / sizeof(T);
+    const int lane = threadIdx.x & 31, b = p.first(), f = p.last();
+    const T* base = src - p.P;
+    if ((b | f) % VEC && b < f) {
+        const int head_end = min((b + VEC - 1) / VEC * VEC, f), tail = max(f / VEC * VEC, head_end), w = b / W + lane;
+        if (w * W < head_end) cp_async4(dst + w * W, base + w * W);
+        if (tail + lane * W < f) cp_async4(dst + tail + lane * W, base + tail + lane * W);
+    }
+}
+// Begins the copy of the warp's part of a slice at src.  16 bytes at a time where src lies P elements behind a 16-byte boundary
+// too, 4 where it lies so behind a 4-byte boundary, else one by one.  Of bf16, the 4 bytes that hold the slice's first or last element may
+// hold one of a neighbour: it is copied too (and covered by end_part).
+template <typename T, int G, int WARPS>
+__device__ __forceinline__ void stage_part(T* dst, const T* src, const Part<G, WARPS>& p) {
+    constexpr int VEC = 16 / sizeof(T), W = 4 / sizeof(T);
+    const int lane = threadIdx.x & 31, b = p.first(), f = p.last();
+    const T* base = src - p.P;
+    if (f <= b) return;
+    if (phase_of(src) == p.P % VEC) {
+        const int first = (b + VEC - 1) / VEC, last = f / VEC;  // whole vectors
+#pragma unroll 4
+        for (int j = first + lane; j < last; j += 32) cp_async16(dst + j * VEC, base + j * VEC);
+        stage_ends(dst, src, p);
+    } else if ((phase_of(src) - p.P) % W == 0) {
+#pragma unroll 8
+        for (int w = b / W + lane; w * W < f; w += 32) cp_async4(dst + w * W, base + w * W);
+    } else {
+        for (int e = b + lane; e < f; e += 32 * 8) {
+            T x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (e + u * 32 < f) x[u] = base[e + u * 32];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (e + u * 32 < f) dst[e + u * 32] = x[u];
+        }
+    }
+}
+// `pad` in the places of the warp's groups that are not the row's.  (Fewer than G + 8 of them; the copies have arrived.)
+template <typename T, int G, int WARPS>
+__device__ __forceinline__ void end_part(T* dst, const Part<G, WARPS>& p, float pad) {
+    const int lane = threadIdx.x & 31, b = p.first(), f = max(p.last(), p.j0 * G);
+    if (p.j0 * G + lane < min(b, p.j1 * G)) dst[p.j0 * G + lane] = from_f<T>(pad);
+    if (f + lane < p.j1 * G) dst[f + lane] = from_f<T>(pad);
+    __syncwarp();
+}
+// f(j, whole) for the warp's groups, one a lane: those that are the row's in whole first, in a loop without a condition.
+template <int G, int WARPS, typename F>
+__device__ __forceinline__ void each_group(const Part<G, WARPS>& p, F&& f) {
+    const int lane = threadIdx.x & 31, inner = p.inner(), outer = p.outer();
+#pragma unroll 4
+    for (int j = inner + lane; j < outer; j += 32) f(j, std::true_type());
+    // of the others, at most two hold some of the row: one in front, one behind
+    if (inner > p.j0 && lane == 0) f(inner - 1, std::false_type());
+    if (outer < p.j1 && lane == 1) f(outer, std::false_type());
+}
+// out[lo, hi) = 0 by a warp.
+template <typename T>
+__device__ __forceinline__ void put_zeros(T* out, int lo, int hi) {
     constexpr int G = 16 / sizeof(T);
     const float zero[G] = {};
-    const int P = phase_of(out);
-    for (int i = (int)threadIdx.x * G - P; i < n; i += THREADS * G) put_at<T, G>(out, i, n, zero);
+    const int lane = threadIdx.x & 31, Pg = (phase_of(out) + lo) % G;
+    for (int e = lo - Pg + lane * G; e < hi; e += 32 * G) put_at<T, G>(out, e, lo, hi, zero);
 }
 
 // ------------------------------------------------------------------ sums of exponentials
@@ -216,10 +312,8 @@ __device__ __forceinline__ float rescale(float from, float to, float c) {
 
 // A sum z of 2^{(x - m) c}, where m is within reach of its largest x (z neither overflows nor vanishes).
 struct Mass {
-    static constexpr int N = 2, SUMS = 1;
     float m, z;
     __device__ __forceinline__ static Mass none() { return {-INFINITY, 0.f}; }
-    __device__ __forceinline__ float* sums() { return &z; }
     __device__ __forceinline__ void raise(Mass& to) const { to.m = fmaxf(to.m, m); }
     __device__ __forceinline__ void share() { m = max_of_warp(m); }
     // against `to`'s reference, which is no less than its own
@@ -234,10 +328,8 @@ __device__ __forceinline__ Mass merge(const Mass& x, const Mass& y, float c) {
 // The masses of two rows s and t over the same entries, and their sums of d = (s - ms) - (t - mt) weighted by each.
 // Against references near the largest of both, d does not grow with what is common to a row.
 struct Pair {
-    static constexpr int N = 6, SUMS = 4;
     float ms, mt, zs, zt, as, at;
     __device__ __forceinline__ static Pair none() { return {-INFINITY, -INFINITY, 0.f, 0.f, 0.f, 0.f}; }
-    __device__ __forceinline__ float* sums() { return &zs; }
     __device__ __forceinline__ void raise(Pair& to) const { to.ms = fmaxf(to.ms, ms), to.mt = fmaxf(to.mt, mt); }
     __device__ __forceinline__ void share() { ms = max_of_warp(ms), mt = max_of_warp(mt); }
     __device__ __forceinline__ Pair against(const Pair& to, float c) const {
@@ -256,24 +348,45 @@ __device__ __forceinline__ float sum_of_warp(float v) {
     return v;
 }
 
-// Places for the sums of a row's warps.
-template <typename S, int THREADS>
-struct Slots {
-    S s[ROW_CTAS * THREADS / 32];
-};
-// A warp's sums (the same in all lanes) to all CTAs of the row (of which there are several: they have waited for one
-// another's start), or to its own.
-template <typename S, int THREADS>
-__device__ __forceinline__ void post(const S& x, Slots<S, THREADS>& slots, int ctas) {
-    constexpr int WARPS = THREADS / 32;
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    if (ctas == 1) {
-        if (lane == 0) slots.s[wid] = x;
-    } else if (lane < ctas) {
-        const uint32_t a = remote_smem(&slots.s[cluster_rank() * WARPS + wid], lane);
-        const float* g = reinterpret_cast<const float*>(&x);
+// Four values' sums at once: lane i gets the sum of v[i / 8].
+__device__ __forceinline__ float sums_of_warp(const float (&v)[4]) {
+    const int lane = threadIdx.x & 31;
+    const bool up = lane & 16, mid = lane & 8;
+    const float a = (up ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[2], 16);
+    const float b = (up ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, up ? v[1] : v[3], 16);
+    float r = (mid ? b : a) + __shfl_xor_sync(0xffffffffu, mid ? a : b, 8);
 #pragma unroll
-        for (int e = 0; e < S::N; ++e) remote_store(a + 4 * e, g[e]);
+    for (int o = 4; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+    return r;
+}
+
+// One float of a warp's sums to its place in this CTA, or in CTA `to` of several (which have waited for one another's start).
+__device__ __forceinline__ void post_float(float* place, int ctas, int to, float v) {
+    if (ctas == 1)
+        *place = v;
+    else
+        remote_store(remote_smem(place, to), v);
+}
+// A warp's sums to its place of `slots` (shared memory for ctas x WARPS of them) in all CTAs of the row; a pair's as each lane's
+// share.
+template <int WARPS>
+__device__ __forceinline__ void post(const Pair& x, Pair* slots, int ctas, int rank) {
+    const int lane = threadIdx.x & 31, to = lane & 7, which = lane >> 3;
+    const float v[4] = {x.zs, x.zt, x.as, x.at};
+    const float sum = sums_of_warp(v);
+    if (to < ctas) {
+        float* f = reinterpret_cast<float*>(slots + rank * WARPS + (threadIdx.x >> 5));
+        post_float(f + 2 + which, ctas, to, sum);
+        if (which < 2) post_float(f + which, ctas, to, which ? x.mt : x.ms);
+    }
+}
+template <int WARPS>
+__device__ __forceinline__ void post(const Mass& x, Mass* slots, int ctas, int rank) {
+    const int lane = threadIdx.x & 31;
+    if (lane < ctas) {
+        float* f = reinterpret_cast<float*>(slots + rank * WARPS + (threadIdx.x >> 5));
+        post_float(f, ctas, lane, x.m);
+        post_float(f + 1, ctas, lane, x.z);
     }
 }
 // All threads of the row: what was posted before is there after it.  In a cluster, none touches the others' shared memory later.
@@ -286,23 +399,31 @@ __device__ __forceinline__ void posted(int ctas) {
         cluster_wait();
     }
 }
-// The row's sums from its warps', the same bits in every thread.
-template <typename S, int THREADS>
-__device__ __forceinline__ S collect(const Slots<S, THREADS>& slots, int ctas, float c) {
-    const int lane = threadIdx.x & 31, count = THREADS / 32 * ctas;
-    S top = S::none();
-    for (int j = lane; j < count; j += 32) slots.s[j].raise(top);
+// The row's sums from its warps', the same bits in every warp that asks.
+__device__ __forceinline__ Mass collect(const Mass* slots, int count, float c) {
+    const int lane = threadIdx.x & 31;
+    Mass top = Mass::none();
+    for (int j = lane; j < count; j += 32) slots[j].raise(top);
     top.share();
-    S r = top;
-#pragma unroll
-    for (int e = 0; e < S::SUMS; ++e) r.sums()[e] = 0.f;
+    float z = 0.f;
+    for (int j = lane; j < count; j += 32) z += slots[j].against(top, c).z;
+    return {top.m, sum_of_warp(z)};
+}
+__device__ __forceinline__ Pair collect(const Pair* slots, int count, float c) {
+    const int lane = threadIdx.x & 31;
+    Pair r = Pair::none();
+    for (int j = lane; j < count; j += 32) slots[j].raise(r);
+    r.share();
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
     for (int j = lane; j < count; j += 32) {
-        S x = slots.s[j].against(top, c);
-#pragma unroll
-        for (int e = 0; e < S::SUMS; ++e) r.sums()[e] += x.sums()[e];
+        const Pair x = slots[j].against(r, c);
+        v[0] += x.zs, v[1] += x.zt, v[2] += x.as, v[3] += x.at;
     }
-#pragma unroll
-    for (int e = 0; e < S::SUMS; ++e) r.sums()[e] = sum_of_warp(r.sums()[e]);
+    const float sum = sums_of_warp(v);
+    r.zs = __shfl_sync(0xffffffffu, sum, 0);
+    r.zt = __shfl_sync(0xffffffffu, sum, 8);
+    r.as = __shfl_sync(0xffffffffu, sum, 16);
+    r.at = __shfl_sync(0xffffffffu, sum, 24);
     return r;
 }
 
@@ -318,6 +439,29 @@ inline cudaError_t allow_row_smem() {
     if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
     e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_SMEM);
     if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+
+// Clusters of `ctas` CTAs that rows are dealt to: no more than run at once.
+template <auto Kernel>
+inline cudaError_t resident_clusters(int ctas, int threads, int per_sm, size_t smem, int64_t rows, int* clusters) {
+    const int sms = device_sm_count();
+    *clusters = (int)std::min<int64_t>(rows, std::max(1, sms * per_sm / ctas));
+    if (ctas <= 2 || rows * ctas <= sms / 2) return cudaSuccess;
+    // larger clusters lie within groups of SMs that they may not fill
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(sms * per_sm / ctas * ctas);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = ctas;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int most = 0;
+    const cudaError_t e = cudaOccupancyMaxActiveClusters(&most, Kernel, &cfg);
+    if (e == cudaSuccess && most > 0) *clusters = std::min(*clusters, most);
     return e;
 }
 
@@ -338,7 +482,7 @@ struct DistillArgs {
     const float* weight;     // [rows] or null
     float* loss;             // [rows] or null
     void* grad;              // rows, or null
-    int V, ctas, slice;
+    int rows, V, ctas, slice;
     float temperature, forward, reverse;
     // the teacher as a list (hbsjd_distill_topk)
     const float* values;     // [rows][k]

@@ -46,31 +46,34 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
             if (key >= lo && key <= hi) atomicAdd(&hist[(key - lo) >> shift], 1u);
         });
         __syncthreads();
-        // every warp: bins from the top, eight per lane
-        uint32_t h[8], sum = 0;
+        if (threadIdx.x < 32) {  // bins from the top, eight per lane
+            uint32_t h[8], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += h[i] = hist[BINS - 1 - (lane * 8 + i)];
-        uint32_t upto = sum;
+            for (int i = 0; i < 8; ++i) sum += h[i] = hist[BINS - 1 - (lane * 8 + i)];
+            uint32_t upto = sum;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
-        }
-        const uint32_t reach = __ballot_sync(0xffffffffu, (int)upto + more >= want);
-        const int at = reach ? __ffs(reach) - 1 : 31;
-        uint32_t before = upto - sum;
-        int bin = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if ((int)before + more < want) {
-                bin = BINS - 1 - (lane * 8 + i);
-                before += h[i];
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += x;
             }
-        bin = __shfl_sync(0xffffffffu, bin, at);
-        const int total = more + (int)__shfl_sync(0xffffffffu, before, at);  // keys that reach the bin
-        const uint32_t start = lo + ((uint32_t)bin << shift);
-        const int inside = (int)hist[bin];
+            const uint32_t reach = __ballot_sync(0xffffffffu, (int)upto + more >= want);
+            if (lane == (reach ? __ffs(reach) - 1 : 31)) {
+                int before = (int)(upto - sum) + more, bin = 0, inside = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (before < want) {
+                        bin = BINS - 1 - (lane * 8 + i);
+                        inside = (int)h[i];
+                        before += inside;
+                    }
+                hist[BINS] = bin;
+                hist[BINS + 1] = before;   // keys that reach the bin
+                hist[BINS + 2] = inside;
+            }
+        }
         __syncthreads();
+        const int total = (int)hist[BINS + 1], inside = (int)hist[BINS + 2];
+        const uint32_t start = lo + (hist[BINS] << shift);
         if (total <= limit || shift == 0) return start;
         more = total - inside;
         hi = min(hi, start + ((1u << shift) - 1));
@@ -83,7 +86,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a, in
     constexpr int G = 16 / sizeof(T), WARPS = THREADS / 32, SETS = 4;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Mass slots[ROW_CTAS], slots_all[WARPS];  // the slices' rests; the warps' of what no list keeps
-    __shared__ uint32_t hist[BINS], red[2][WARPS];
+    __shared__ uint32_t hist[BINS + 3], red[2][WARPS];
     __shared__ float sums[WARPS];
     __shared__ int found;
     pdl_wait();
@@ -103,10 +106,14 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a, in
     T* xs = (T*)smem;
     unsigned long long* cand = (unsigned long long*)(smem + (a.slice + 16) * sizeof(T));
     unsigned long long* lists = cand + cap;  // [ctas][k], several CTAs only
-    stage_row<T, G, THREADS>(xs, src, n, P, -INFINITY);
+    stage_row<T, THREADS>(xs, src, n, P);
     if (tid == 0) found = 0;
     cp_async_wait_all();
     __syncthreads();
+    if ((P + n) % G || P) {
+        end_row<T, G>(xs, n, P, -INFINITY);
+        __syncthreads();
+    }
 
     // ---- a bound that at least k entries reach
     uint32_t thr = LOWEST_KEY;
