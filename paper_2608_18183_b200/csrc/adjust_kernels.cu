@@ -14,7 +14,23 @@ namespace hbsjd {
 namespace {
 
 constexpr int AD_THREADS = 256;
-constexpr int AD_GROUPS = 4;  // 16-byte groups of a thread: all of a CTA's logits are on their way while it counts the history
+#ifndef ADG
+#define ADG 2
+#endif
+constexpr int AD_GROUPS = ADG;  // 16-byte groups of a thread: all of a CTA's logits are on their way while it counts the history
+
+// (volatile: the loads of all groups are to be under way before the first is used)
+__device__ __forceinline__ uint4 load16(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ float element(const uint4& v, int i) {
+    if (sizeof(T) == 4) return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w);
+    const uint32_t w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
+    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+}
 
 // x[i] is entry v + i of the row; those outside [0, V) are not looked at (v may be negative).
 template <int G>
@@ -63,8 +79,7 @@ __device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t*
             if (!(m >> i & 1)) x[i] = -INFINITY;
     }
 #pragma unroll
-    for (int i = 0; i < G; ++i)
-        if (x[i] != x[i]) x[i] = -INFINITY;
+    for (int i = 0; i < G; ++i) x[i] = fmaxf(x[i], -INFINITY);  // (of NaN and a number, the number)
 }
 
 template <typename T, bool GUIDED>
@@ -82,18 +97,13 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
     // groups of 16 bytes of the output; P + n <= chunk + G - 1 elements, so a chunk of whole rounds has one group more at most
     const int P = phase_of(out), rounds = (P + n + AD_THREADS * G - 1) / (AD_THREADS * G);
     const bool wide = phase_of(x) == P && (!GUIDED || phase_of(u) == P);
-    float f[AD_GROUPS][G];
+    uint4 f[AD_GROUPS], g[GUIDED ? AD_GROUPS : 1];
 #pragma unroll
     for (int r = 0; r < AD_GROUPS; ++r) {
         const int e = (r * AD_THREADS + tid) * G - P;
         if (wide && e >= 0 && e + G <= n) {
-            get<G>(x + e, f[r]);
-            if (GUIDED) {
-                float g[G];
-                get<G>(u + e, g);
-#pragma unroll
-                for (int i = 0; i < G; ++i) f[r][i] = fmaf(a.cfg_scale, f[r][i] - g[i], g[i]);
-            }
+            f[r] = load16(x + e);
+            if (GUIDED) g[r] = load16(u + e);
         }
     }
     const uint32_t* bits = nullptr;
@@ -110,9 +120,13 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
             for (int i = tid * 4; i < P + n; i += AD_THREADS * 4) *reinterpret_cast<int4*>(count + i) = make_int4(0, 0, 0, 0);
             __syncthreads();
             const int32_t* tok = a.history + h * a.ld_history;
-            for (int i = tid; i < len; i += AD_THREADS) {
-                const int64_t e = (int64_t)tok[i] - v0;
-                if (e >= 0 && e < n) atomicAdd(&count[P + e], 1);
+            for (int i0 = tid; i0 < len; i0 += AD_THREADS * 8) {
+                int32_t t[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) t[i] = i0 + i * AD_THREADS < len ? tok[i0 + i * AD_THREADS] : -1;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (t[i] >= v0 && t[i] < v0 + n) atomicAdd(&count[P + t[i] - v0], 1);
             }
             __syncthreads();
             counts = count;
@@ -126,7 +140,14 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
         float y[G];
         if (r < AD_GROUPS && wide && e >= 0 && e + G <= n) {
 #pragma unroll
-            for (int i = 0; i < G; ++i) y[i] = f[r < AD_GROUPS ? r : 0][i];
+            for (int i = 0; i < G; ++i) y[i] = element<T>(f[r < AD_GROUPS ? r : 0], i);
+            if (GUIDED) {
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    const float z = element<T>(g[r < AD_GROUPS ? r : 0], i);
+                    y[i] = fmaf(a.cfg_scale, y[i] - z, z);
+                }
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < G; ++i) {

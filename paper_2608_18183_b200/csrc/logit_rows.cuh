@@ -500,7 +500,7 @@ struct TopkArgs {
     float* values;     // [rows][k]
     int32_t* indices;  // [rows][k]
     float* rest;       // [rows] or null
-    int V, k, ctas, slice;
+    int rows, V, k, ctas, slice, cap;
     float temperature;
     // rows of a scoring forward (null: row r of x is row r of the outputs): row r holds the distribution of position
     // at[r].y + 1 of image at[r].x, and goes to row at[r].x * T + at[r].y if that position lies behind the image's prefix

@@ -32,7 +32,8 @@ __device__ __forceinline__ unsigned long long rank_key(float x, int index) {
 }
 
 // A bound for the `want`-th largest of the keys that visit(f) hands to f: all threads get a key that at least `want` keys reach,
-// and at most `limit` if that can be had; else the want-th largest itself.  No key lies beyond hi, and at least `want` reach lo.
+// and at most `limit` if that can be had; else the want-th largest itself.  No key lies beyond hi, and at least `want` reach lo.  The
+// bins are clear, and all threads have met since.
 template <int THREADS, typename Visit>
 __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want, int limit, uint32_t* hist,
                                               Visit&& visit) {
@@ -40,8 +41,6 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
     int more = 0;
     while (true) {
         const int shift = max(0, 24 - __clz(hi - lo));  // (hi - lo) >> shift < BINS
-        for (int i = threadIdx.x; i < BINS; i += THREADS) hist[i] = 0;
-        __syncthreads();
         visit([&](uint32_t key) {
             if (key >= lo && key <= hi) atomicAdd(&hist[(key - lo) >> shift], 1u);
         });
@@ -75,346 +74,443 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
         const int total = (int)hist[BINS + 1], inside = (int)hist[BINS + 2];
         const uint32_t start = lo + (hist[BINS] << shift);
         if (total <= limit || shift == 0) return start;
+        for (int i = threadIdx.x; i < BINS; i += THREADS) hist[i] = 0;
+        __syncthreads();
         more = total - inside;
         hi = min(hi, start + ((1u << shift) - 1));
         lo = start;
     }
 }
 
+// key[0, size), a power of two up to THREADS, by size, largest first: a bitonic network whose steps within a warp are shuffles (10
+// of the 45 steps of 512 keys are not).  To be followed by no barrier.
+template <int THREADS>
+__device__ __forceinline__ void sort_descending(unsigned long long* key, int size) {
+    const int tid = threadIdx.x;
+    const bool mine = (tid & ~31) < size;
+    unsigned long long x = tid < size ? key[tid] : 0;
+    for (int span = 2; span <= size; span *= 2)
+        for (int o = span / 2; o > 0; o /= 2) {
+            unsigned long long y = 0;
+            if (o >= 32) {
+                __syncthreads();
+                if (mine) key[tid] = x;
+                __syncthreads();
+                if (mine) y = key[tid ^ o];
+            } else if (mine) {
+                y = __shfl_xor_sync(0xffffffffu, x, o);
+            }
+            const bool larger = ((tid & o) == 0) == ((tid & span) == 0);
+            x = (x > y) == larger ? x : y;
+        }
+    __syncthreads();
+    if (tid < size) key[tid] = x;
+    __syncthreads();
+}
+
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a, int cap) {
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
     constexpr int G = 16 / sizeof(T), WARPS = THREADS / 32, SETS = 4;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ Mass slots[ROW_CTAS], slots_all[WARPS];  // the slices' rests; the warps' of what no list keeps
-    __shared__ uint32_t hist[BINS + 3], red[2][WARPS];
+    __shared__ Mass rests[ROW_CTAS];  // of the slices
+    __shared__ uint32_t hist[BINS + 3], red[3][WARPS];
     __shared__ float sums[WARPS];
-    __shared__ int found;
+    __shared__ int noted, found, bad, big;  // groups with candidates; candidates; a sum that is no number; one that is far from zero
     pdl_wait();
     pdl_trigger();
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, k = a.k;
-    const int64_t row = blockIdx.x / a.ctas;
-    int64_t to = row;
-    if (a.at) {
-        const int2 at = __ldcg(a.at + row);
-        if (at.x < 0 || at.y < a.prefix_len[at.x]) return;
-        to = (int64_t)at.x * a.T + at.y;
-    }
-    if (a.ctas > 1) cluster_arrive();
-    const int rank = blockIdx.x % a.ctas, v0 = rank * a.slice, n = max(0, min(a.slice, a.V - v0));
-    const T* src = (const T*)a.x + row * a.ld + v0;
-    const int P = phase_of(src), groups = (P + n + G - 1) / G;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, k = a.k, cap = a.cap;
+    const int rank = blockIdx.x % a.ctas, v0 = rank * a.slice, n = max(0, min(a.slice, a.V - v0)), step = gridDim.x / a.ctas;
+    const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
+    const f32x2 c2 = both(c);
     T* xs = (T*)smem;
-    unsigned long long* cand = (unsigned long long*)(smem + (a.slice + 16) * sizeof(T));
-    unsigned long long* lists = cand + cap;  // [ctas][k], several CTAs only
-    stage_row<T, THREADS>(xs, src, n, P);
-    if (tid == 0) found = 0;
-    cp_async_wait_all();
-    __syncthreads();
-    if ((P + n) % G || P) {
-        end_row<T, G>(xs, n, P, -INFINITY);
-        __syncthreads();
+    unsigned long long* cand = (unsigned long long*)(smem + (a.slice + 16) * sizeof(T));  // [cap]
+    unsigned long long* other = cand + cap;                                              // [cap] in order, or
+    int32_t* notes = (int32_t*)other;                                                    // [2 cap] groups
+    unsigned long long* lists = other + cap;  // [ctas][k], several CTAs only
+    if (tid == 0) found = noted = bad = big = 0;
+    if (a.ctas > 1) {
+        cluster_arrive();
+        cluster_wait();  // every CTA of the rows runs
     }
+    const auto source = [&](int row) { return (const T*)a.x + (int64_t)row * a.ld + v0; };
+    // where a row's results go, -1: nowhere
+    const auto target = [&](int row) -> int64_t {
+        if (row >= a.rows) return -1;
+        if (!a.at) return row;
+        const int2 at = __ldcg(a.at + row);
+        return at.x < 0 || at.y < __ldg(a.prefix_len + at.x) ? -1 : (int64_t)at.x * a.T + at.y;
+    };
+    int row = blockIdx.x / a.ctas;
+    int64_t to = target(row);
+    if (to >= 0) stage_row<T, THREADS>(xs, source(row), n, phase_of(source(row)));
+    for (; row < a.rows; row += step) {
+        const int64_t to1 = target(row + step);
+        bool fetched = to1 < 0;
+        const auto fetch = [&] {
+            if (!fetched) stage_row<T, THREADS>(xs, source(row + step), n, phase_of(source(row + step)));
+            fetched = true;
+        };
+        if (to < 0) {  // (all CTAs of the row)
+            fetch();
+            to = to1;
+            continue;
+        }
+        const int P = phase_of(source(row)), groups = (P + n + G - 1) / G;
+        cp_async_wait_all();
+        for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;
+        __syncthreads();
+        if ((P + n) % G || P) {
+            end_row<T, G>(xs, n, P, -INFINITY);
+            __syncthreads();
+        }
+        const auto each = [&](auto&& f) {
+#pragma unroll 4
+            for (int j = tid; j < groups; j += THREADS) {
+                float x[G];
+                get<G>(xs + j * G, x);
+                f(x, j);
+            }
+        };
 
-    // ---- a bound that at least k entries reach
-    uint32_t thr = LOWEST_KEY;
-    uint32_t top = 0;
-    if (n > cap) {
-        float best[SETS];
+        // ---- a bound that at least k entries reach
+        uint32_t thr = LOWEST_KEY, top = 0;
+        if (n > cap) {
+            float best[SETS];
 #pragma unroll
-        for (int i = 0; i < SETS; ++i) best[i] = -INFINITY;
-        for (int j0 = tid; j0 < groups; j0 += THREADS * SETS) {
+            for (int i = 0; i < SETS; ++i) best[i] = -INFINITY;
+            int j = tid;
+            for (; j + (SETS - 1) * THREADS < groups; j += THREADS * SETS) {
 #pragma unroll
-            for (int u = 0; u < SETS; ++u) {
-                const int j = j0 + u * THREADS;
-                if (j < groups) {
+                for (int u = 0; u < SETS; ++u) {
                     float x[G];
-                    get<G>(xs + j * G, x);
+                    get<G>(xs + (j + u * THREADS) * G, x);
 #pragma unroll
                     for (int i = 0; i < G; ++i) best[u] = fmaxf(best[u], x[i]);
                 }
             }
-        }
-        int sets = SETS;
-        if (k * 4 <= THREADS) {  // enough threads: one set each
-            best[0] = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
-            sets = 1;
-        }
-        uint32_t key[SETS], lo = 0xffffffffu;
-        int filled = 0;
 #pragma unroll
-        for (int i = 0; i < SETS; ++i) {
-            key[i] = key_of(best[i]);
-            if (i < sets && key[i] >= LOWEST_KEY) {
-                lo = min(lo, key[i]);
-                top = max(top, key[i]);
-                ++filled;
+            for (int u = 0; u < SETS - 1; ++u)
+                if (j + u * THREADS < groups) {
+                    float x[G];
+                    get<G>(xs + (j + u * THREADS) * G, x);
+#pragma unroll
+                    for (int i = 0; i < G; ++i) best[u] = fmaxf(best[u], x[i]);
+                }
+            int sets = SETS;
+            if (k * 4 <= THREADS) {  // enough threads: one set each
+                best[0] = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
+                sets = 1;
             }
+            uint32_t key[SETS], lo = 0xffffffffu;
+            int filled = 0;
+#pragma unroll
+            for (int i = 0; i < SETS; ++i) {
+                key[i] = key_of(best[i]);
+                if (i < sets && key[i] >= LOWEST_KEY) {
+                    lo = min(lo, key[i]);
+                    top = max(top, key[i]);
+                    ++filled;
+                }
+            }
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            top = __reduce_max_sync(0xffffffffu, top);
+            filled = __reduce_add_sync(0xffffffffu, filled);
+            if (lane == 0) {
+                red[0][wid] = lo;
+                red[1][wid] = top;
+                red[2][wid] = filled;
+            }
+            __syncthreads();
+            lo = __reduce_min_sync(0xffffffffu, red[0][lane % WARPS]);
+            top = __reduce_max_sync(0xffffffffu, red[1][lane % WARPS]);
+            filled = __reduce_add_sync(0xffffffffu, lane < WARPS ? red[2][lane % WARPS] : 0);
+            if (filled >= k)
+                thr = bound_key<THREADS>(lo, top, k, k + max(16, k / 4), hist, [&](auto&& f) {
+#pragma unroll
+                    for (int i = 0; i < SETS; ++i)
+                        if (i < sets) f(key[i]);
+                });
         }
-        lo = __reduce_min_sync(0xffffffffu, lo);
-        top = __reduce_max_sync(0xffffffffu, top);
-        filled = __reduce_add_sync(0xffffffffu, filled);
-        if (lane == 0) {
-            red[0][wid] = lo;
-            red[1][wid] = top;
-            hist[wid] = filled;
-        }
-        __syncthreads();
-        lo = __reduce_min_sync(0xffffffffu, red[0][lane % WARPS]);
-        top = __reduce_max_sync(0xffffffffu, red[1][lane % WARPS]);
-        filled = __reduce_add_sync(0xffffffffu, lane < WARPS ? hist[lane % WARPS] : 0);
-        __syncthreads();  // (hist is cleared next)
-        if (filled >= k)
-            thr = bound_key<THREADS>(lo, top, k, k + max(16, k / 4), hist, [&](auto&& f) {
+        // ---- candidates, and the mass of all others against the bound
+        bool tied = false;  // too many entries equal the k-th: only those beyond it are candidates yet
+        int reach = 0;      // (if so) the entries that reach it
+        while (true) {
+            const float t = value_of(thr);
+            const f32x2 o = both(-t);
+            f32x2 z2 = both(0.f);
+            each([&](float(&x)[G], int j) {
+                float most = x[0];
 #pragma unroll
-                for (int i = 0; i < SETS; ++i)
-                    if (i < sets) f(key[i]);
-            });
-    }
-    // ---- candidates, and the mass of all others against the bound
-    const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
-    const f32x2 c2 = both(c);
-    float z, t;
-    bool tied = false;  // too many entries equal the k-th: only those beyond it are candidates yet
-    int reach = 0;      // (if so) the entries that reach it
-    while (true) {
-        t = value_of(thr);
-        const f32x2 o = both(-t);
-        f32x2 z2 = both(0.f);
-        for (int j = tid; j < groups; j += THREADS) {
-            float x[G];
-            get<G>(xs + j * G, x);
-            float most = x[0];
-#pragma unroll
-            for (int i = 1; i < G; ++i) most = fmaxf(most, x[i]);
-            if (most >= t) {
-#pragma unroll
-                for (int i = 0; i < G; ++i)
-                    if (x[i] >= t) {
-                        if (!tied || x[i] > t) {
-                            const int p = atomicAdd(&found, 1);
-                            if (p < cap) cand[p] = rank_key(x[i], v0 + j * G + i - P);
-                        }
-                        x[i] = -INFINITY;
+                for (int i = 1; i < G; ++i) most = fmaxf(most, x[i]);
+                // A group that reaches the bound is only noted: some lane of a warp has one in half of the steps and more.
+                if (most >= t) {
+                    if (!tied || most > t) {
+                        const int p = atomicAdd(&noted, 1);
+                        if (p < 2 * cap) notes[p] = j;
                     }
-            }
-            if (a.rest) {
 #pragma unroll
-                for (int i = 0; i < G; i += 2) z2 = add2(z2, ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)));
+                    for (int i = 0; i < G; ++i) x[i] = x[i] >= t ? -INFINITY : x[i];
+                }
+                if (a.rest) {
+#pragma unroll
+                    for (int i = 0; i < G; i += 2) z2 = add2(z2, ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)));
+                }
+            });
+            const float z = sum_of_warp(sum2(z2));
+            if (lane == 0) {
+                sums[wid] = z;
+                if (!(z < 1e20f)) bad = 1;
+                if (z > 1e-20f) big = 1;
             }
-        }
-        z = sum2(z2);
-        __syncthreads();
-        if (found <= cap) break;
-        // the entries that reach the bound, narrowed until they fit; the k-th largest itself if they never do
-        __syncthreads();
-        if (tid == 0) found = 0;
-        thr = bound_key<THREADS>(thr, top, k, cap, hist, [&](auto&& f) {
-            for (int j = tid; j < groups; j += THREADS) {
+            __syncthreads();
+            const int groups_noted = noted;
+            for (int q = tid; q < min(groups_noted, 2 * cap); q += THREADS) {
+                const int j = notes[q];
                 float x[G];
                 get<G>(xs + j * G, x);
 #pragma unroll
                 for (int i = 0; i < G; ++i)
-                    if (x[i] > -INFINITY) f(key_of(x[i]));
-            }
-        });
-        // (where more than cap entries reach it still, it is the k-th largest: fewer than k lie above)
-        reach = 0;
-        const float u = value_of(thr);
-        for (int j = tid; j < groups; j += THREADS) {
-            float x[G];
-            get<G>(xs + j * G, x);
-#pragma unroll
-            for (int i = 0; i < G; ++i) reach += x[i] >= u;
-        }
-        reach = __reduce_add_sync(0xffffffffu, reach);
-        if (lane == 0) red[0][wid] = reach;
-        __syncthreads();
-        reach = __reduce_add_sync(0xffffffffu, lane < WARPS ? red[0][lane % WARPS] : 0);
-        tied = reach > cap;
-        __syncthreads();
-    }
-    int count = found;
-    if (tied) {  // the first of the tied entries, by index
-        for (int e0 = 0; e0 < P + n && count < k; e0 += THREADS) {
-            const int e = e0 + tid;
-            const bool is = e < P + n && to_f<T>(xs[e]) == t;
-            const uint32_t b = __ballot_sync(0xffffffffu, is);
-            if (lane == 0) red[0][wid] = __popc(b);
-            __syncthreads();
-            int place = count + __popc(b & ((1u << lane) - 1)), all = 0;
-            for (int w = 0; w < WARPS; ++w) {
-                if (w < wid) place += red[0][w];
-                all += red[0][w];
-            }
-            if (is && place < k) cand[place] = rank_key(t, v0 + e - P);
-            count = min(k, count + all);
-            __syncthreads();
-        }
-        if (tid == 0) z += (float)(reach - count);  // those that were not taken
-    }
-    __syncthreads();
-
-    // ---- order
-    float* values = a.values + to * k;
-    int32_t* indices = a.indices + to * k;
-    const auto place = [&](int r, unsigned long long key) {
-        if (a.ctas == 1) {
-            values[r] = key ? value_of((uint32_t)(key >> 32)) : -INFINITY;
-            indices[r] = key ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
-        } else {
-            remote_store(remote_smem(lists + rank * k + r, 0), key);
-        }
-    };
-    if (a.ctas > 1) cluster_wait();  // every CTA of the row runs
-    const unsigned long long* sorted = cand;
-    if ((int64_t)count * count <= 128 * THREADS) {
-        int per = 1;  // threads per candidate
-        while (per < 32 && per * 2 * count <= THREADS) per *= 2;
-        const int i = tid / per;
-        const unsigned long long key = i < count ? cand[i] : 0;
-        int r = 0;
-        for (int j = tid % per; j < count; j += per) r += cand[j] > key;
-        for (int o = 1; o < per; o <<= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
-        // (cand holds 1024 or more, count is at most 256: the atomics' order ends here)
-        if (i < count && tid % per == 0) cand[512 + r] = key;
-        sorted = cand + 512;
-        __syncthreads();
-    } else {
-        int size = 1;
-        while (size < count) size *= 2;
-        for (int i = count + tid; i < size; i += THREADS) cand[i] = 0;
-        for (int span = 2; span <= size; span *= 2)
-            for (int o = span / 2; o > 0; o /= 2) {
-                __syncthreads();
-                for (int p = tid; p < size / 2; p += THREADS) {
-                    const int i = 2 * o * (p / o) + p % o;
-                    const unsigned long long x = cand[i], y = cand[i + o];
-                    if ((x < y) == ((i & span) == 0)) {
-                        cand[i] = y;
-                        cand[i + o] = x;
+                    if (x[i] >= t && (!tied || x[i] > t)) {
+                        const int p = atomicAdd(&found, 1);
+                        if (p < cap) cand[p] = rank_key(x[i], v0 + j * G + i - P);
                     }
-                }
             }
-        __syncthreads();
-    }
-    // (where every entry is a candidate, none was summed yet, and the bound is no entry)
-    if (thr == LOWEST_KEY && count > k) t = value_of((uint32_t)(sorted[k - 1] >> 32));
-    for (int i = tid; i < max(count, k); i += THREADS)
-        if (i < k)
-            place(i, i < count ? sorted[i] : 0);
-        else  // a candidate behind the k-th
-            z += ex2((value_of((uint32_t)(sorted[i] >> 32)) - t) * c);
-
-    // ---- the rest
-    Mass rest = {t, 0.f};
-    if (a.rest) {
-        z = sum_of_warp(z);
-        if (lane == 0) sums[wid] = z;
-        __syncthreads();
-        rest.z = sum_of_warp(lane < WARPS ? sums[lane % WARPS] : 0.f);
-        // NaN in the row, or all of the rest far off the bound: again, against its largest and passing NaN over
-        if (!(rest.z > 1e-20f && rest.z < 1e20f)) {
-            const auto each = [&](auto&& f) {
-                for (int j = tid; j < groups; j += THREADS) {
-                    float x[G];
-                    get<G>(xs + j * G, x);
+            __syncthreads();
+            if (found <= cap && groups_noted <= 2 * cap) break;
+            // the entries that reach the bound, narrowed until they fit; the k-th largest itself if they never do
+            for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;
+            __syncthreads();
+            if (tid == 0) found = noted = bad = big = 0;
+            thr = bound_key<THREADS>(thr, top, k, cap, hist, [&](auto&& f) {
+                each([&](const float(&x)[G], int) {
 #pragma unroll
                     for (int i = 0; i < G; ++i)
-                        if (x[i] < value_of(thr)) f(x[i], 1.f);
-                }
-                for (int i = k + tid; i < count; i += THREADS) f(value_of((uint32_t)(sorted[i] >> 32)), 1.f);
-                if (tied && tid == 0 && reach > count) f(t, (float)(reach - count));
-            };
-            float m = -INFINITY;
-            each([&](float x, float) { m = fmaxf(m, x); });
+                        if (x[i] > -INFINITY) f(key_of(x[i]));
+                });
+            });
+            // (where more than cap entries reach it still, it is the k-th largest: fewer than k lie above)
+            reach = 0;
+            const float u = value_of(thr);
+            each([&](const float(&x)[G], int) {
+#pragma unroll
+                for (int i = 0; i < G; ++i) reach += x[i] >= u;
+            });
+            reach = __reduce_add_sync(0xffffffffu, reach);
+            if (lane == 0) red[0][wid] = reach;
+            __syncthreads();
+            reach = __reduce_add_sync(0xffffffffu, lane < WARPS ? red[0][lane % WARPS] : 0);
+            tied = reach > cap;
+            __syncthreads();
+        }
+        int count = found;
+        float t = value_of(thr), zr = -1.f;  // reference of the sum; the sum itself where it was taken again
+        if (a.rest && (bad || !(big || thr == LOWEST_KEY))) {
+            // NaN in the row, or all others far off the bound: again, against their largest and passing NaN over
+            const float least = t;
+            float m = -INFINITY, z = 0.f;
+            each([&](const float(&x)[G], int) {
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+                    if (x[i] < least) m = fmaxf(m, x[i]);
+            });
             m = max_of_warp(m);
             __syncthreads();
             if (lane == 0) sums[wid] = m;
             __syncthreads();
             m = max_of_warp(sums[lane % WARPS]);
-            z = 0.f;
-            const float o = m == -INFINITY ? 0.f : m;
-            each([&](float x, float times) { z += x == m ? times : times * ex2((x - o) * c); });
+            if (m > -INFINITY) {
+                each([&](const float(&x)[G], int) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i)
+                        if (x[i] < least) z += ex2((x[i] - m) * c);
+                });
+                t = m;
+            }
             z = sum_of_warp(z);
             __syncthreads();
             if (lane == 0) sums[wid] = z;
             __syncthreads();
-            rest = {m, m == -INFINITY ? 0.f : sum_of_warp(lane < WARPS ? sums[lane % WARPS] : 0.f)};
+            zr = sum_of_warp(lane < WARPS ? sums[lane % WARPS] : 0.f);
+            if (tied && zr > 0.f) zr *= rescale(t, least, c);  // (the tied entries join it)
+            if (tied) t = least;
         }
-    }
-    if (a.ctas > 1) {
-        if (tid == 0) {
-            const uint32_t place = remote_smem(&slots[rank], 0);
-            remote_store(place, rest.m);
-            remote_store(place + 4, rest.z);
-        }
-        posted(a.ctas);
-        if (rank) return;
-        // the lists of all slices: an entry's place is its own list's and, for each other, the entries that come first
-        Mass mine = Mass::none();
-        int valid = 0;
-        for (int i = tid; i < a.ctas * k; i += THREADS) {
-            const unsigned long long key = lists[i];
-            if (!key) continue;
-            ++valid;
-            int r = i % k;
-            for (int l = 0; l < a.ctas; ++l) {
-                if (l == i / k) continue;
-                const unsigned long long* list = lists + l * k;
-                int first = 0, last = k;  // entries before `first` are larger, those from `last` on are not
-                while (first < last) {
-                    const int mid = (first + last) / 2;
-                    if (list[mid] > key)
-                        first = mid + 1;
-                    else
-                        last = mid;
+        if (tied) {  // the first of the tied entries, by index
+            const float u = value_of(thr);
+            for (int e0 = 0; e0 < P + n && count < k; e0 += THREADS) {
+                const int e = e0 + tid;
+                const bool is = e < P + n && to_f<T>(xs[e]) == u;
+                const uint32_t b = __ballot_sync(0xffffffffu, is);
+                if (lane == 0) red[0][wid] = __popc(b);
+                __syncthreads();
+                int place = count + __popc(b & ((1u << lane) - 1)), all = 0;
+                for (int w = 0; w < WARPS; ++w) {
+                    if (w < wid) place += red[0][w];
+                    all += red[0][w];
                 }
-                r += first;
+                if (is && place < k) cand[place] = rank_key(u, v0 + e - P);
+                count = min(k, count + all);
+                __syncthreads();
             }
-            if (r < k) {
-                values[r] = value_of((uint32_t)(key >> 32));
-                indices[r] = (int32_t)(0xffffffffu - (uint32_t)key);
+        }
+        if (tied) __syncthreads();
+        fetch();  // the row is read
+
+        // ---- order
+        const unsigned long long* sorted = cand;
+        if (count <= THREADS / 2 && count * count <= 64 * THREADS) {
+            // few: an entry's place is how many are before it
+            int per = 1;  // threads per candidate
+            while (per < 32 && per * 2 * count <= THREADS) per *= 2;
+            const int i = tid / per;
+            const uint32_t lanes = __ballot_sync(0xffffffffu, i < count);
+            if (i < count) {
+                const unsigned long long key = cand[i];
+                int r = 0;
+#pragma unroll 4
+                for (int j = tid % per; j < count; j += per) r += cand[j] > key;
+                for (int o = 1; o < per; o <<= 1) r += __shfl_xor_sync(lanes, r, o);
+                if (tid % per == 0) other[r] = key;
+            }
+            sorted = other;
+            __syncthreads();
+        } else {
+            int size = 1;
+            while (size < count) size *= 2;
+            for (int i = count + tid; i < size; i += THREADS) cand[i] = 0;
+            __syncthreads();
+            if (size <= THREADS) {
+                sort_descending<THREADS>(cand, size);
             } else {
-                mine = merge(mine, {value_of((uint32_t)(key >> 32)), 1.f}, c);
+                for (int span = 2; span <= size; span *= 2)
+                    for (int o = span / 2; o > 0; o /= 2) {
+                        for (int p = tid; p < size / 2; p += THREADS) {
+                            const int i = 2 * o * (p / o) + p % o;
+                            const unsigned long long x = cand[i], y = cand[i + o];
+                            if ((x < y) == ((i & span) == 0)) {
+                                cand[i] = y;
+                                cand[i + o] = x;
+                            }
+                        }
+                        __syncthreads();
+                    }
             }
         }
-        valid = __reduce_add_sync(0xffffffffu, valid);
-        if (lane == 0) red[0][wid] = valid;
-        if (tid < a.ctas) mine = merge(mine, slots[tid], c);
-        Mass all = mine;
-        all.share();
-        all.z = sum_of_warp(mine.against(all, c).z);
-        if (lane == 0) slots_all[wid] = all;
-        __syncthreads();
-        mine = lane < WARPS ? slots_all[lane] : Mass::none();
-        rest = mine;
-        rest.share();
-        rest.z = sum_of_warp(mine.against(rest, c).z);
-        valid = __reduce_add_sync(0xffffffffu, lane < WARPS ? red[0][lane % WARPS] : 0);
-        for (int i = valid + tid; i < k; i += THREADS) {
-            values[i] = -INFINITY;
-            indices[i] = -1;
+        if (tid == 0) found = noted = bad = big = 0;
+        float* values = a.values + to * k;
+        int32_t* indices = a.indices + to * k;
+        for (int i = tid; i < k; i += THREADS) {
+            const unsigned long long key = i < count ? sorted[i] : 0;
+            if (a.ctas == 1) {
+                values[i] = key ? value_of((uint32_t)(key >> 32)) : -INFINITY;
+                indices[i] = key ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
+            } else {
+                remote_store(remote_smem(lists + rank * k + i, 0), key);
+            }
         }
+        // ---- the rest: the sum over the row, and the candidates behind the k-th, against the largest
+        Mass rest = {t, 0.f};
+        if (wid == 0 && a.rest) {
+            rest.z = zr >= 0.f ? zr : sum_of_warp(lane < WARPS ? sums[lane % WARPS] : 0.f);
+            if (tied) rest.z += (float)(reach - count);
+            if (count > k) {
+                const float m = value_of((uint32_t)(sorted[k] >> 32));
+                float z = 0.f;
+                for (int i = k + lane; i < count; i += 32) {
+                    const float x = value_of((uint32_t)(sorted[i] >> 32));
+                    z += x == m ? 1.f : ex2((x - m) * c);
+                }
+                if (rest.z > 0.f) rest.z *= rescale(t, m, c);
+                rest = {m, sum_of_warp(z) + rest.z};
+            }
+            if (rest.z == 0.f) rest.m = -INFINITY;
+        }
+        if (a.ctas == 1) {
+            if (a.rest && tid == 0) a.rest[to] = rest.z == 0.f ? -INFINITY : fmaf(rest.m, inv_tau, LN2 * lg2(rest.z));
+        } else {
+            if (tid == 0) {
+                const uint32_t place = remote_smem(&rests[rank], 0);
+                remote_store(place, rest.m);
+                remote_store(place + 4, rest.z);
+            }
+            posted(a.ctas);
+            if (rank == 0) {
+                // the lists of all slices: an entry's place is its own list's and, for each other, the entries that come first
+                Mass mine = tid < a.ctas ? rests[tid] : Mass::none();
+                int valid = 0;
+                for (int i = tid; i < a.ctas * k; i += THREADS) {
+                    const unsigned long long key = lists[i];
+                    if (!key) continue;
+                    ++valid;
+                    int r = i % k;
+                    for (int l = 0; l < a.ctas; ++l) {
+                        if (l == i / k) continue;
+                        const unsigned long long* list = lists + l * k;
+                        int first = 0, last = k;  // entries before `first` are larger, those from `last` on are not
+                        while (first < last) {
+                            const int mid = (first + last) / 2;
+                            if (list[mid] > key)
+                                first = mid + 1;
+                            else
+                                last = mid;
+                        }
+                        r += first;
+                    }
+                    if (r < k) {
+                        values[r] = value_of((uint32_t)(key >> 32));
+                        indices[r] = (int32_t)(0xffffffffu - (uint32_t)key);
+                    } else {
+                        mine = merge(mine, {value_of((uint32_t)(key >> 32)), 1.f}, c);
+                    }
+                }
+                valid = __reduce_add_sync(0xffffffffu, valid);
+                Mass all = mine;
+                all.share();
+                all.z = sum_of_warp(mine.against(all, c).z);
+                if (lane == 0) {
+                    red[0][wid] = valid;
+                    red[1][wid] = __float_as_uint(all.m);
+                    sums[wid] = all.z;
+                }
+                __syncthreads();
+                mine = lane < WARPS ? Mass{__uint_as_float(red[1][lane % WARPS]), sums[lane % WARPS]} : Mass::none();
+                rest = mine;
+                rest.share();
+                rest.z = sum_of_warp(mine.against(rest, c).z);
+                valid = __reduce_add_sync(0xffffffffu, lane < WARPS ? red[0][lane % WARPS] : 0);
+                for (int i = valid + tid; i < k; i += THREADS) {
+                    values[i] = -INFINITY;
+                    indices[i] = -1;
+                }
+                if (a.rest && tid == 0) a.rest[to] = rest.z == 0.f ? -INFINITY : fmaf(rest.m, inv_tau, LN2 * lg2(rest.z));
+            }
+            // (the others' lists of the next row are to wait for these)
+            cluster_arrive();
+            cluster_wait();
+        }
+        to = to1;
     }
-    if (a.rest && tid == 0)
-        a.rest[to] = rest.z == 0.f ? -INFINITY : fmaf(rest.m, inv_tau, LN2 * log2f(rest.z));
 }
 
 template <typename T>
-cudaError_t run_topk(const TopkArgs& a, int rows, Stream& s) {
+cudaError_t run_topk(TopkArgs& a, Stream& s) {
     constexpr int G = 16 / sizeof(T);
-    int cap = 1024;
-    while (cap < 4 * a.k) cap *= 2;
-    const size_t smem = (a.slice + 16) * sizeof(T) + cap * 8 + (a.ctas > 1 ? (size_t)a.ctas * a.k * 8 : 0);
+    a.cap = 512;
+    while (a.cap < 2 * a.k) a.cap *= 2;
+    const size_t smem = (a.slice + 16) * sizeof(T) + a.cap * 16 + (a.ctas > 1 ? (size_t)a.ctas * a.k * 8 : 0);
     const auto run = [&](auto threads) {
         constexpr int THREADS = decltype(threads)::value;
-        const cudaError_t e = allow_row_smem<k_topk<T, THREADS>>();
+        cudaError_t e = allow_row_smem<k_topk<T, THREADS>>();
         if (e != cudaSuccess) return e;
-        return launch_kc(true, k_topk<T, THREADS>, dim3((unsigned)rows * a.ctas), dim3(THREADS), smem, s, a.ctas, a, cap);
+        const int per_sm = std::max(1, std::min<int>(1536 / THREADS, 227 * 1024 / (smem + 1024 + 1600)));  // (1 KB is the system's)
+        int clusters = 0;
+        e = resident_clusters<k_topk<T, THREADS>>(a.ctas, THREADS, per_sm, smem, a.rows, &clusters);
+        if (e != cudaSuccess) return e;
+        return launch_kc(true, k_topk<T, THREADS>, dim3((unsigned)clusters * a.ctas), dim3(THREADS), smem, s, a.ctas, a);
     };
     // at least eight groups a thread, and two maxima per entry of the list
-    if (a.slice <= 8 * 128 * G && a.k <= 256) return run(std::integral_constant<int, 128>());
-    if (a.slice <= 8 * 256 * G && a.k <= 512) return run(std::integral_constant<int, 256>());
+    const int per = (getenv("HB_PER") ? atoi(getenv("HB_PER")) : 8) * G;
+    if (a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
+    if (a.slice <= 256 * per && a.k <= 512) return run(std::integral_constant<int, 256>());
     return run(std::integral_constant<int, 512>());
 }
 
@@ -423,8 +519,8 @@ cudaError_t run_topk(const TopkArgs& a, int rows, Stream& s) {
 cudaError_t launch_topk(const TopkArgs& args, int rows, int dtype, Stream& s) {
     TopkArgs a = args;
     const RowSplit sp = split_row(rows, a.V, dtype ? 2 : 4, device_sm_count());
-    a.ctas = sp.ctas, a.slice = sp.slice;
-    return dtype ? run_topk<bf16>(a, rows, s) : run_topk<float>(a, rows, s);
+    a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice;
+    return dtype ? run_topk<bf16>(a, s) : run_topk<float>(a, s);
 }
 
 }  // namespace hbsjd
