@@ -1,21 +1,23 @@
 // The K largest logits of a row, in order, and the logarithm of the mass of all others: what of a teacher's distribution is
 // stored for a student.
 //
-// One CTA (or a cluster, see below) holds a row in shared memory.  Selection: a thread keeps the maxima of its own groups of
-// entries; a key that K of these maxima reach is a lower bound for the K-th largest entry and close to it (512 groups of 32 of
-// 16384 normal entries: 68 candidates for K = 64).  It comes from histograms of 256 bins over the maxima's keys, which narrow
-// to one bin until few maxima are too many.  One more pass collects the candidates and sums the exponentials of all others
-// against the bound, the candidates are ranked by counting or sorted, and those behind the K-th join the sum.  No difference
-// of masses is taken: the rest keeps its digits however small it is.  Candidates that do not fit (an order of the row that puts
-// the largest into few groups, ties without end) are narrowed by histograms over the entries themselves.
-// A row is read from HBM once, which bounds the kernel.  The CTAs of a cluster select from their slices; the first merges the lists.
+// A CTA (or a cluster, see below) holds a row in shared memory.  Selection: a thread keeps the maximum of its own entries (or four, of
+// parts of them); a key that k of these maxima reach is a lower bound for the k-th largest entry and close to it (256 maxima of 64
+// of 16384 normal entries: 84 candidates for k = 64).  It comes from histograms of 256 bins over the maxima's keys, which narrow
+// to one bin until few maxima are too many.  One more pass marks the groups with candidates and sums the exponentials of all others
+// against the bound; the candidates go into bins over their own range, and those of one bin are counted against one another.  No
+// difference of masses is taken: the rest keeps its digits however small it is.  Candidates that do not fit (an order of the row that
+// puts the largest into few threads' entries, ties without end) are narrowed by histograms over the entries themselves.
+// A row is read from HBM once; the barriers between these steps and their latency bound the kernel (three CTAs an SM, 17000 cycles
+// a row of 16384 fp32, of which HBM would need 8500).  The next row is fetched while the list is put in order.  The CTAs of
+// a cluster select from their slices; the first merges the lists.
 #include "logit_rows.cuh"
 
 namespace hbsjd {
 
 namespace {
 
-constexpr int BINS = 256;
+constexpr int BINS = 256;  // (eight per lane of the warp that scans them)
 constexpr uint32_t LOWEST_KEY = 0x00800000u;  // of the lowest finite value; -inf and NaN lie below
 
 // Order of the values as whole numbers; -0 counts as 0.
@@ -82,32 +84,6 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
     }
 }
 
-// key[0, size), a power of two up to THREADS, by size, largest first: a bitonic network whose steps within a warp are shuffles (10
-// of the 45 steps of 512 keys are not).  To be followed by no barrier.
-template <int THREADS>
-__device__ __forceinline__ void sort_descending(unsigned long long* key, int size) {
-    const int tid = threadIdx.x;
-    const bool mine = (tid & ~31) < size;
-    unsigned long long x = tid < size ? key[tid] : 0;
-    for (int span = 2; span <= size; span *= 2)
-        for (int o = span / 2; o > 0; o /= 2) {
-            unsigned long long y = 0;
-            if (o >= 32) {
-                __syncthreads();
-                if (mine) key[tid] = x;
-                __syncthreads();
-                if (mine) y = key[tid ^ o];
-            } else if (mine) {
-                y = __shfl_xor_sync(0xffffffffu, x, o);
-            }
-            const bool larger = ((tid & o) == 0) == ((tid & span) == 0);
-            x = (x > y) == larger ? x : y;
-        }
-    __syncthreads();
-    if (tid < size) key[tid] = x;
-    __syncthreads();
-}
-
 template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
     constexpr int G = 16 / sizeof(T), WARPS = THREADS / 32, SETS = 4;
@@ -115,7 +91,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
     __shared__ Mass rests[ROW_CTAS];  // of the slices
     __shared__ uint32_t hist[BINS + 3], red[3][WARPS];
     __shared__ float sums[WARPS];
-    __shared__ int noted, found, bad, big;  // groups with candidates; candidates; a sum that is no number; one that is far from zero
+    __shared__ int found, bad, big;        // candidates; a sum that is no number; one that is far from zero
+    __shared__ uint32_t least_key, top_key;  // of the candidates
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, k = a.k, cap = a.cap;
@@ -124,10 +101,12 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
     const f32x2 c2 = both(c);
     T* xs = (T*)smem;
     unsigned long long* cand = (unsigned long long*)(smem + (a.slice + 16) * sizeof(T));  // [cap]
-    unsigned long long* other = cand + cap;                                              // [cap] in order, or
-    int32_t* notes = (int32_t*)other;                                                    // [2 cap] groups
+    unsigned long long* other = cand + cap;   // [cap]
     unsigned long long* lists = other + cap;  // [ctas][k], several CTAs only
-    if (tid == 0) found = noted = bad = big = 0;
+    if (tid == 0) {
+        found = bad = big = 0;
+        least_key = 0xffffffffu, top_key = 0;
+    }
     if (a.ctas > 1) {
         cluster_arrive();
         cluster_wait();  // every CTA of the rows runs
@@ -238,49 +217,79 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
             const float t = value_of(thr);
             const f32x2 o = both(-t);
             f32x2 z2 = both(0.f);
-            each([&](float(&x)[G], int j) {
+            // A group that reaches the bound is only marked: some lane of a warp has one in half of the steps and more.
+            uint32_t marks = 0;
+            int step_no = 0;
+            each([&](const float(&x)[G], int) {
                 float most = x[0];
 #pragma unroll
                 for (int i = 1; i < G; ++i) most = fmaxf(most, x[i]);
-                // A group that reaches the bound is only noted: some lane of a warp has one in half of the steps and more.
-                if (most >= t) {
-                    if (!tied || most > t) {
-                        const int p = atomicAdd(&noted, 1);
-                        if (p < 2 * cap) notes[p] = j;
-                    }
-#pragma unroll
-                    for (int i = 0; i < G; ++i) x[i] = x[i] >= t ? -INFINITY : x[i];
-                }
+                if (most >= t) marks |= 1u << step_no;
+                ++step_no;
                 if (a.rest) {
+                    f32x2 e = both(0.f);
 #pragma unroll
-                    for (int i = 0; i < G; i += 2) z2 = add2(z2, ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)));
+                    for (int i = 0; i < G; i += 2) e = add2(e, ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)));
+                    if (!(most >= t)) z2 = add2(z2, e);
                 }
             });
-            const float z = sum_of_warp(sum2(z2));
+            float z = sum2(z2);
+            // The marked groups of a warp, a lane each, from a list of its own (in `other`, which is free here).
+            uint16_t* list = (uint16_t*)other + wid * 64;
+            for (int listed = 0;;) {
+                uint32_t more = __ballot_sync(0xffffffffu, marks != 0);
+                while (more && listed < 32) {
+                    if (marks) list[listed + __popc(more & ((1u << lane) - 1))] = (uint16_t)(tid + (__ffs(marks) - 1) * THREADS);
+                    marks &= marks - 1;
+                    listed += __popc(more);
+                    more = __ballot_sync(0xffffffffu, marks != 0);
+                }
+                if (!listed) break;
+                __syncwarp();
+                const int take = min(listed, 32);
+                listed -= take;
+                if (lane < take) {
+                    const int j = list[listed + lane];
+                    float x[G], lo = INFINITY, hi = -INFINITY;
+                    get<G>(xs + j * G, x);
+                    int some = 0;
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        const bool in = x[i] >= t, kept = in && (!tied || x[i] > t);
+                        if (!in) z += ex2((x[i] - t) * c);
+                        some += kept;
+                        lo = kept ? fminf(lo, x[i]) : lo;
+                        hi = kept ? fmaxf(hi, x[i]) : hi;
+                    }
+                    if (some) {
+                        int p = atomicAdd(&found, some);
+                        atomicMin(&least_key, key_of(lo));
+                        atomicMax(&top_key, key_of(hi));
+#pragma unroll
+                        for (int i = 0; i < G; ++i)
+                            if (x[i] >= t && (!tied || x[i] > t)) {
+                                if (p < cap) cand[p] = rank_key(x[i], v0 + j * G + i - P);
+                                ++p;
+                            }
+                    }
+                }
+                __syncwarp();
+            }
+            z = sum_of_warp(z);
             if (lane == 0) {
                 sums[wid] = z;
                 if (!(z < 1e20f)) bad = 1;
                 if (z > 1e-20f) big = 1;
             }
+            for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;  // (for the order; the bound's were read before threads last met)
             __syncthreads();
-            const int groups_noted = noted;
-            for (int q = tid; q < min(groups_noted, 2 * cap); q += THREADS) {
-                const int j = notes[q];
-                float x[G];
-                get<G>(xs + j * G, x);
-#pragma unroll
-                for (int i = 0; i < G; ++i)
-                    if (x[i] >= t && (!tied || x[i] > t)) {
-                        const int p = atomicAdd(&found, 1);
-                        if (p < cap) cand[p] = rank_key(x[i], v0 + j * G + i - P);
-                    }
-            }
-            __syncthreads();
-            if (found <= cap && groups_noted <= 2 * cap) break;
+            if (found <= cap) break;
             // the entries that reach the bound, narrowed until they fit; the k-th largest itself if they never do
-            for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;
             __syncthreads();
-            if (tid == 0) found = noted = bad = big = 0;
+            if (tid == 0) {
+                found = bad = big = 0;
+                least_key = 0xffffffffu, top_key = 0;
+            }
             thr = bound_key<THREADS>(thr, top, k, cap, hist, [&](auto&& f) {
                 each([&](const float(&x)[G], int) {
 #pragma unroll
@@ -352,50 +361,61 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
                 __syncthreads();
             }
         }
-        if (tied) __syncthreads();
+        if (tied) {
+            if (tid == 0) least_key = thr, top_key = max(top_key, thr);
+            for (int i = tid; i < BINS; i += THREADS) hist[i] = 0;
+            __syncthreads();
+        }
         fetch();  // the row is read
 
         // ---- order
-        const unsigned long long* sorted = cand;
-        if (count <= THREADS / 2 && count * count <= 64 * THREADS) {
-            // few: an entry's place is how many are before it
-            int per = 1;  // threads per candidate
-            while (per < 32 && per * 2 * count <= THREADS) per *= 2;
-            const int i = tid / per;
-            const uint32_t lanes = __ballot_sync(0xffffffffu, i < count);
-            if (i < count) {
-                const unsigned long long key = cand[i];
-                int r = 0;
-#pragma unroll 4
-                for (int j = tid % per; j < count; j += per) r += cand[j] > key;
-                for (int o = 1; o < per; o <<= 1) r += __shfl_xor_sync(lanes, r, o);
-                if (tid % per == 0) other[r] = key;
-            }
-            sorted = other;
+        // By bins over the candidates' keys (and tokens, where all are equal): what is in a higher bin comes first, those of one bin
+        // are counted against one another.
+        if (count > 1) {
+            const uint32_t least = least_key;
+            const auto place_of = [&](unsigned long long key) {  // value, then token, in the bits that differ
+                return (unsigned long long)((uint32_t)(key >> 32) - least) << 17 | ((uint32_t)key & 0x1ffffu);
+            };
+            const int shift = max(0, 64 - __clzll((unsigned long long)(top_key - least) << 17 | 0x1ffffu) - 8);
+            for (int q = tid; q < count; q += THREADS) atomicAdd(&hist[place_of(cand[q]) >> shift], 1u);
             __syncthreads();
-        } else {
-            int size = 1;
-            while (size < count) size *= 2;
-            for (int i = count + tid; i < size; i += THREADS) cand[i] = 0;
-            __syncthreads();
-            if (size <= THREADS) {
-                sort_descending<THREADS>(cand, size);
-            } else {
-                for (int span = 2; span <= size; span *= 2)
-                    for (int o = span / 2; o > 0; o /= 2) {
-                        for (int p = tid; p < size / 2; p += THREADS) {
-                            const int i = 2 * o * (p / o) + p % o;
-                            const unsigned long long x = cand[i], y = cand[i + o];
-                            if ((x < y) == ((i & span) == 0)) {
-                                cand[i] = y;
-                                cand[i + o] = x;
-                            }
-                        }
-                        __syncthreads();
-                    }
+            if (tid < 32) {  // how many are in higher bins; eight bins per lane, from the top
+                uint32_t h[8], sum = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum += h[i] = hist[BINS - 1 - (lane * 8 + i)];
+                uint32_t upto = sum;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+                    if (lane >= o) upto += x;
+                }
+                upto -= sum;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    hist[BINS - 1 - (lane * 8 + i)] = upto;
+                    upto += h[i];
+                }
             }
+            __syncthreads();
+            for (int q = tid; q < count; q += THREADS) {
+                const unsigned long long key = cand[q];
+                other[atomicAdd(&hist[place_of(key) >> shift], 1u)] = key;
+            }
+            __syncthreads();
+            for (int q = tid; q < count; q += THREADS) {
+                const unsigned long long key = other[q];
+                const int bin = (int)(place_of(key) >> shift), first = bin == BINS - 1 ? 0 : (int)hist[bin + 1], last = (int)hist[bin];
+                int r = first;
+                for (int j = first; j < last; ++j) r += other[j] > key;
+                cand[r] = key;
+            }
+            __syncthreads();
         }
-        if (tid == 0) found = noted = bad = big = 0;
+        const unsigned long long* sorted = cand;
+        if (tid == 0) {
+            found = bad = big = 0;
+            least_key = 0xffffffffu, top_key = 0;
+        }
         float* values = a.values + to * k;
         int32_t* indices = a.indices + to * k;
         for (int i = tid; i < k; i += THREADS) {
@@ -507,8 +527,9 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
         if (e != cudaSuccess) return e;
         return launch_kc(true, k_topk<T, THREADS>, dim3((unsigned)clusters * a.ctas), dim3(THREADS), smem, s, a.ctas, a);
     };
-    // at least eight groups a thread, and two maxima per entry of the list
-    const int per = (getenv("HB_PER") ? atoi(getenv("HB_PER")) : 8) * G;
+    // Sixteen groups a thread at least, as for the divergences (lists of 64 from 8192 rows of 16384 fp32: 148 us with 256 threads, 185
+    // with 512), four where there are few rows; and two maxima per entry of the list.
+    const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? 16 : 4) * G;
     if (a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
     if (a.slice <= 256 * per && a.k <= 512) return run(std::integral_constant<int, 256>());
     return run(std::integral_constant<int, 512>());
