@@ -14,10 +14,37 @@ namespace hbsjd {
 namespace {
 
 constexpr int AD_THREADS = 256;
-#ifndef ADG
-#define ADG 2
-#endif
-constexpr int AD_GROUPS = ADG;  // 16-byte groups of a thread: all of a CTA's logits are on their way while it counts the history
+constexpr int AD_AHEAD = 2;  // groups of 16 bytes that a thread has on their way
+
+// How often the tokens of a chunk occur, in shared memory: 16 bits each where no history is longer than they count to.
+template <typename C>
+struct Counts {
+    static constexpr int PER = 4 / sizeof(C);  // in a word
+    __device__ __forceinline__ static void add(uint32_t* table, int e) { atomicAdd(table + e / PER, 1u << (e % PER * 16)); }
+    // of G entries from e on, a multiple of G; false if there are none
+    template <int G>
+    __device__ __forceinline__ static bool get(const uint32_t* table, int e, float (&n)[G]) {
+        uint32_t w[G / PER], any = 0;
+        const uint32_t* p = table + e / PER;
+        if constexpr (G / PER == 2) {
+            const uint2 q = *reinterpret_cast<const uint2*>(p);
+            w[0] = q.x, w[1] = q.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < G / PER; i += 4) {
+                const uint4 q = *reinterpret_cast<const uint4*>(p + i);
+                w[i] = q.x, w[i + 1] = q.y, w[i + 2] = q.z, w[i + 3] = q.w;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < G / PER; ++i) any |= w[i];
+        if (!any) return false;
+#pragma unroll
+        for (int i = 0; i < G; ++i)  // (16 bits become fp32 as the low ones of 2^23 + n: one step that is no conversion)
+            n[i] = PER == 1 ? (float)w[i] : __uint_as_float(__byte_perm(w[i / 2], 0x4b00u, i % 2 ? 0x5432 : 0x5410)) - 8388608.f;
+        return true;
+    }
+};
 
 // (volatile: the loads of all groups are to be under way before the first is used)
 __device__ __forceinline__ uint4 load16(const void* p) {
@@ -33,26 +60,16 @@ __device__ __forceinline__ float element(const uint4& v, int i) {
 }
 
 // x[i] is entry v + i of the row; those outside [0, V) are not looked at (v may be negative).
-template <int G>
-__device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t* bits, const int32_t* counts, float (&x)[G], int v,
-                                            int e) {
-    if (counts) {
-        int n[G];
-        bool any = false;
+template <int G, typename C>
+__device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t* bits, const uint32_t* counts, float inv, float (&x)[G],
+                                            int v, int e) {
+    float n[G];
+    if (counts && Counts<C>::template get<G>(counts, e, n)) {
+        // (without a branch: some lane of a warp has such a token nearly always)
 #pragma unroll
-        for (int i = 0; i < G; i += 4) {
-            const int4 q = *reinterpret_cast<const int4*>(counts + e + i);
-            n[i] = q.x, n[i + 1] = q.y, n[i + 2] = q.z, n[i + 3] = q.w;
-            any |= (q.x | q.y | q.z | q.w) != 0;
-        }
-        if (any) {
-            // (without a branch: some lane of a warp has such a token nearly always)
-            const float inv = 1.f / a.repetition;
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-                const float y = x[i] * (x[i] > 0.f ? inv : a.repetition) - fmaf((float)n[i], a.frequency, a.presence);
-                x[i] = n[i] ? y : x[i];
-            }
+        for (int i = 0; i < G; ++i) {
+            const float y = x[i] * (x[i] > 0.f ? inv : a.repetition) - fmaf(n[i], a.frequency, a.presence);
+            x[i] = n[i] > 0.f ? y : x[i];
         }
     }
     if (a.bias) {
@@ -63,6 +80,9 @@ __device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t*
                 const float4 q = __ldg(reinterpret_cast<const float4*>(b + i));
                 x[i] += q.x, x[i + 1] += q.y, x[i + 2] += q.z, x[i + 3] += q.w;
             }
+        } else if (v >= 0 && v + G <= a.V) {
+#pragma unroll
+            for (int i = 0; i < G; ++i) x[i] += __ldg(b + i);
         } else {
 #pragma unroll
             for (int i = 0; i < G; ++i)
@@ -82,7 +102,7 @@ __device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t*
     for (int i = 0; i < G; ++i) x[i] = fmaxf(x[i], -INFINITY);  // (of NaN and a number, the number)
 }
 
-template <typename T, bool GUIDED>
+template <typename T, bool GUIDED, typename C>
 __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, int chunks) {
     constexpr int G = 16 / sizeof(T);
     extern __shared__ __align__(16) unsigned char smem[];
@@ -91,91 +111,101 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x / chunks;
     const int v0 = blockIdx.x % chunks * chunk, n = min(chunk, a.V - v0);
+    // what the row has of its own, asked for first: the history's tokens wait for it
+    const int which = a.mask && a.mask_row ? a.mask_row[row] : 0;
+    const int64_t h = a.history && a.history_row ? a.history_row[row] : row;
+    int len = !a.history ? 0 : min(a.history_len ? a.history_len[row] : a.history_cap, a.history_cap);
     const T* x = (const T*)a.x + row * a.ld + v0;
     const T* u = (const T*)a.u + (GUIDED ? row * a.ld_u + v0 : 0);
     T* out = (T*)a.out + row * a.ld_out + v0;
-    // groups of 16 bytes of the output; P + n <= chunk + G - 1 elements, so a chunk of whole rounds has one group more at most
-    const int P = phase_of(out), rounds = (P + n + AD_THREADS * G - 1) / (AD_THREADS * G);
+    // groups of 16 bytes of the output: the entry of a thread's first, and the entries from one to its next
+    const int P = phase_of(out), e0 = tid * G - P;
+    constexpr int STEP = AD_THREADS * G;
     const bool wide = phase_of(x) == P && (!GUIDED || phase_of(u) == P);
-    uint4 f[AD_GROUPS], g[GUIDED ? AD_GROUPS : 1];
-#pragma unroll
-    for (int r = 0; r < AD_GROUPS; ++r) {
-        const int e = (r * AD_THREADS + tid) * G - P;
+    uint4 f[AD_AHEAD], g[AD_AHEAD];
+    const auto load = [&](int slot, int e) {
         if (wide && e >= 0 && e + G <= n) {
-            f[r] = load16(x + e);
-            if (GUIDED) g[r] = load16(u + e);
+            f[slot] = load16(x + e);
+            if (GUIDED) g[slot] = load16(u + e);
         }
-    }
-    const uint32_t* bits = nullptr;
-    if (a.mask) {
-        const int m = a.mask_row ? a.mask_row[row] : 0;
-        if (m >= 0 && m < a.masks) bits = a.mask + m * a.ld_mask;
-    }
-    const int32_t* counts = nullptr;
-    if (a.history) {
-        const int64_t h = a.history_row ? a.history_row[row] : row;
-        const int len = min(a.history_len ? a.history_len[row] : a.history_cap, a.history_cap);
-        if (h >= 0 && h < a.histories && len > 0) {
-            int32_t* count = (int32_t*)smem;  // element P is the chunk's first
-            for (int i = tid * 4; i < P + n; i += AD_THREADS * 4) *reinterpret_cast<int4*>(count + i) = make_int4(0, 0, 0, 0);
-            __syncthreads();
-            const int32_t* tok = a.history + h * a.ld_history;
-            for (int i0 = tid; i0 < len; i0 += AD_THREADS * 8) {
-                int32_t t[8];
+    };
 #pragma unroll
-                for (int i = 0; i < 8; ++i) t[i] = i0 + i * AD_THREADS < len ? tok[i0 + i * AD_THREADS] : -1;
+    for (int i = 0; i < AD_AHEAD; ++i) load(i, e0 + i * STEP);
+    const uint32_t* bits = a.mask && which >= 0 && which < a.masks ? a.mask + which * a.ld_mask : nullptr;
+    const uint32_t* counts = nullptr;
+    if (h < 0 || h >= a.histories) len = 0;
+    if (len > 0) {
+        uint32_t* table = (uint32_t*)smem;  // element P is the chunk's first
+        for (int i = tid * 16; i < (P + n + G) * (int)sizeof(C); i += AD_THREADS * 16) *reinterpret_cast<uint4*>(smem + i) = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+        const int32_t* tok = a.history + h * a.ld_history;
+        for (int i0 = tid; i0 < len; i0 += AD_THREADS * 8) {
+            int32_t t[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (t[i] >= v0 && t[i] < v0 + n) atomicAdd(&count[P + t[i] - v0], 1);
-            }
-            __syncthreads();
-            counts = count;
+            for (int i = 0; i < 8; ++i) t[i] = i0 + i * AD_THREADS < len ? tok[i0 + i * AD_THREADS] : -1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (t[i] >= v0 && t[i] < v0 + n) Counts<C>::add(table, P + t[i] - v0);
         }
+        __syncthreads();
+        counts = table;
     }
+    const float inv = 1.f / a.repetition;
+    for (int e = e0; e < n;) {
 #pragma unroll
-    for (int r = 0; r < AD_GROUPS + 1; ++r) {
-        if (r >= rounds) break;
-        const int e = (r * AD_THREADS + tid) * G - P;
-        if (e >= n) break;
-        float y[G];
-        if (r < AD_GROUPS && wide && e >= 0 && e + G <= n) {
+        for (int slot = 0; slot < AD_AHEAD; ++slot, e += STEP) {
+            if (e >= n) break;
+            float y[G];
+            if (wide && e >= 0 && e + G <= n) {
 #pragma unroll
-            for (int i = 0; i < G; ++i) y[i] = element<T>(f[r < AD_GROUPS ? r : 0], i);
-            if (GUIDED) {
+                for (int i = 0; i < G; ++i) y[i] = element<T>(f[slot], i);
+                if (GUIDED) {
+#pragma unroll
+                    for (int i = 0; i < G; ++i) {
+                        const float z = element<T>(g[slot], i);
+                        y[i] = fmaf(a.cfg_scale, y[i] - z, z);
+                    }
+                }
+            } else {
 #pragma unroll
                 for (int i = 0; i < G; ++i) {
-                    const float z = element<T>(g[r < AD_GROUPS ? r : 0], i);
-                    y[i] = fmaf(a.cfg_scale, y[i] - z, z);
+                    const bool in = e + i >= 0 && e + i < n;
+                    y[i] = in ? to_f<T>(x[e + i]) : 0.f;
+                    if (GUIDED && in) y[i] = fmaf(a.cfg_scale, y[i] - to_f<T>(u[e + i]), to_f<T>(u[e + i]));
                 }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < G; ++i) {
-                const bool in = e + i >= 0 && e + i < n;
-                y[i] = in ? to_f<T>(x[e + i]) : 0.f;
-                if (GUIDED && in) y[i] = fmaf(a.cfg_scale, y[i] - to_f<T>(u[e + i]), to_f<T>(u[e + i]));
-            }
+            load(slot, e + AD_AHEAD * STEP);
+            apply_rules<G, C>(a, bits, counts, inv, y, v0 + e, P + e);
+            put_at<T, G>(out, e, 0, n, y);
         }
-        apply_rules<G>(a, bits, counts, y, v0 + e, P + e);
-        put_at<T, G>(out, e, 0, n, y);
     }
 }
 
-template <typename T, bool GUIDED>
+template <typename T, bool GUIDED, typename C>
 cudaError_t run_adjust(const AdjustArgs& a, int rows, Stream& s) {
     constexpr int G = 16 / sizeof(T);
-    int chunk = AD_THREADS * G * AD_GROUPS;
+    const cudaError_t e = allow_row_smem<k_adjust<T, GUIDED, C>>();
+    if (e != cudaSuccess) return e;
+    // Every chunk reads the row's whole history, and its table takes shared memory: 4096 guided rows of 16384 fp32 with histories of 256
+    // take 138, 131 and 162 us with chunks of 4096, 8192 and 16384 entries, 771 rows of 50021 bf16 with histories of up to 4096
+    // 77, 63 and 68.  Smaller chunks where rows are few.
+    int chunk = 8192;
     while (chunk > AD_THREADS * G && (int64_t)rows * ((a.V + chunk - 1) / chunk) < 2 * device_sm_count()) chunk /= 2;
     const int chunks = (a.V + chunk - 1) / chunk;
-    const size_t smem = a.history ? (min(chunk, a.V) + 16) * sizeof(int32_t) : 0;
-    return launch_k(k_adjust<T, GUIDED>, dim3((unsigned)rows * chunks), dim3(AD_THREADS), smem, s, a, chunk, chunks);
+    const size_t smem = a.history ? ((size_t)std::min(chunk, a.V) + 32) * sizeof(C) : 0;
+    return launch_k(k_adjust<T, GUIDED, C>, dim3((unsigned)rows * chunks), dim3(AD_THREADS), smem, s, a, chunk, chunks);
+}
+
+template <typename T>
+cudaError_t run_adjust(const AdjustArgs& a, int rows, Stream& s) {
+    if (a.history_cap > 0xffff) return a.u ? run_adjust<T, true, uint32_t>(a, rows, s) : run_adjust<T, false, uint32_t>(a, rows, s);
+    return a.u ? run_adjust<T, true, uint16_t>(a, rows, s) : run_adjust<T, false, uint16_t>(a, rows, s);
 }
 
 }  // namespace
 
 cudaError_t launch_adjust(const AdjustArgs& a, int rows, int dtype, Stream& s) {
-    if (a.u) return dtype ? run_adjust<bf16, true>(a, rows, s) : run_adjust<float, true>(a, rows, s);
-    return dtype ? run_adjust<bf16, false>(a, rows, s) : run_adjust<float, false>(a, rows, s);
+    return dtype ? run_adjust<bf16>(a, rows, s) : run_adjust<float>(a, rows, s);
 }
 
 }  // namespace hbsjd

@@ -78,14 +78,12 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
             Pair v = Pair::none();
             {
                 float x[G], y[G];
-                if (p.j0 + lane < p.j1) {
-                    get<G>(ss + (p.j0 + lane) * G, x);
-                    get<G>(st + (p.j0 + lane) * G, y);
+                const int sample = p.inner() + lane;
+                if (sample < p.outer()) {
+                    get<G>(ss + sample * G, x);
+                    get<G>(st + sample * G, y);
 #pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        const int e = (p.j0 + lane) * G + i;
-                        if (e >= p.P && e < p.P + n) v.ms = fmaxf(v.ms, x[i]), v.mt = fmaxf(v.mt, y[i]);
-                    }
+                    for (int i = 0; i < G; ++i) v.ms = fmaxf(v.ms, x[i]), v.mt = fmaxf(v.mt, y[i]);
                 }
                 v.share();
                 const f32x2 os = both(-v.ms), ot = both(-v.mt), c2 = both(c), minus = both(-1.f);
@@ -359,13 +357,11 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
             Mass u = Mass::none();
             {
                 float x[G];
-                if (p.j0 + lane < p.j1) {
-                    get<G>(ss + (p.j0 + lane) * G, x);
+                const int sample = p.inner() + lane;
+                if (sample < p.outer()) {
+                    get<G>(ss + sample * G, x);
 #pragma unroll
-                    for (int i = 0; i < G; ++i) {
-                        const int e = (p.j0 + lane) * G + i;
-                        if (e >= p.P && e < p.P + n) u.m = fmaxf(u.m, x[i]);
-                    }
+                    for (int i = 0; i < G; ++i) u.m = fmaxf(u.m, x[i]);
                 }
                 u.share();
                 const f32x2 o = both(-u.m), c2 = both(c);
