@@ -384,6 +384,16 @@ typedef struct {
 int hbsjd_topk_logits(void *cuda_stream, const hbsjd_topk_desc *d, const void *logits, float *values, int32_t *indices,
                       float *rest);
 
+/* The lists of a model's distributions over completed trajectories: what hbsjd_distill_topk needs of a teacher, at 8 k + 4 bytes
+ * a position in place of 4 V (Sec. 4.1, Eq. 3: teacher and student read the same tokens).  The model of context c runs
+ * the forwards of hbsjd_score; entry [b, t - 1] of the outputs is the distribution of position t given x_<t, for the positions
+ * t > prefix_len[b] (the others get empty lists: hbsjd_distill_topk leaves them out).
+ *   tokens DEVICE int32 [batch, T], prefix_len, class_labels DEVICE int32 [batch]: as hbsjd_score
+ *   values DEVICE fp32 [batch, T, k], indices DEVICE int32 [batch, T, k], rest DEVICE fp32 [batch, T] or NULL: as hbsjd_topk_logits
+ * Runs on the context's stream and waits; its rollout state and KV caches are overwritten.  Errors as hbsjd_score. */
+int hbsjd_score_topk(hbsjd_ctx *c, int batch, const int32_t *tokens, const int32_t *prefix_len, const int32_t *class_labels, int k,
+                     float temperature, float *values, int32_t *indices, float *rest);
+
 /* Divergence of the student's distribution q = softmax(logits_s / temperature) from the teacher's p and its gradient:
  *   loss[r] = forward KL(p || q) + reverse KL(q || p);   grad[r] = weight[r] d loss[r] / d logits_s[r]
  * forward = reverse = 1/2 at temperature 1 is Eq. 3, as hbsjd_bikl computes it.

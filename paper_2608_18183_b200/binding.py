@@ -21,7 +21,8 @@ EXPORTS = ["hbsjd_create", "hbsjd_rollout", "hbsjd_prefill_passes", "hbsjd_rollo
            "hbsjd_set_state", "hbsjd_debug_read", "hbsjd_debug_forward", "hbsjd_debug_gemm",
            "hbsjd_debug_shuffle_pages", "hbsjd_debug_fold_norm", "hbsjd_debug_fail_round",
            "hbsjd_debug_force_tile", "hbsjd_gemm", "hbsjd_bikl", "hbsjd_score", "hbsjd_strerror",
-           "hbsjd_last_error", "hbsjd_adjust_logits", "hbsjd_topk_logits", "hbsjd_distill", "hbsjd_distill_topk"]
+           "hbsjd_last_error", "hbsjd_adjust_logits", "hbsjd_topk_logits", "hbsjd_distill", "hbsjd_distill_topk",
+           "hbsjd_score_topk"]
 
 
 class hbsjd_model_desc(C.Structure):
@@ -134,6 +135,7 @@ def load():
         L.hbsjd_topk_logits.argtypes = [vp, C.POINTER(hbsjd_topk_desc)] + [vp] * 4
         L.hbsjd_distill.argtypes = [vp, C.POINTER(hbsjd_distill_desc)] + [vp] * 5
         L.hbsjd_distill_topk.argtypes = [vp, C.POINTER(hbsjd_distill_desc)] + [vp] * 7
+        L.hbsjd_score_topk.argtypes = [vp, C.c_int, vp, vp, vp, C.c_int, C.c_float, vp, vp, vp]
         L.hbsjd_strerror.argtypes = [C.c_int]
         L.hbsjd_strerror.restype = C.c_char_p
         L.hbsjd_last_error.argtypes = [vp]
@@ -581,6 +583,23 @@ class Context:
         self.batch = 0
         teacher.batch = 0
         return pos, per, loss.value
+
+    def hbsjd_score_topk(self, tokens, prefix_len, class_labels, k, temperature=1.0):
+        """The k largest logits of this model at every position of completed trajectories: (values fp32 [batch, T, k],
+        indices int32 [batch, T, k], rest fp32 [batch, T]), device tensors; empty lists for the prefixes."""
+        torch = self._torch
+        batch, T = tokens.shape[0], self.shape.T
+        assert tokens.is_cuda and tokens.dtype == torch.int32 and tokens.is_contiguous()
+        assert tuple(tokens.shape) == (batch, T)
+        assert prefix_len.dtype == torch.int32 and class_labels.dtype == torch.int32
+        values = torch.empty((batch, T, k), dtype=torch.float32, device=tokens.device)
+        indices = torch.empty((batch, T, k), dtype=torch.int32, device=tokens.device)
+        rest = torch.empty((batch, T), dtype=torch.float32, device=tokens.device)
+        self._check(self.lib.hbsjd_score_topk(self.h, batch, tokens.data_ptr(), prefix_len.data_ptr(),
+                                              class_labels.data_ptr(), k, temperature, values.data_ptr(),
+                                              indices.data_ptr(), rest.data_ptr()), "hbsjd_score_topk")
+        self.batch = 0
+        return values, indices, rest
 
     def hbsjd_destroy(self):
         if self.h:

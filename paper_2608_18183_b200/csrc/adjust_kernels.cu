@@ -80,9 +80,17 @@ __device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t*
                 const float4 q = __ldg(reinterpret_cast<const float4*>(b + i));
                 x[i] += q.x, x[i + 1] += q.y, x[i + 2] += q.z, x[i + 3] += q.w;
             }
-        } else if (v >= 0 && v + G <= a.V) {
+        } else if (v >= 3 && v + G + 3 <= a.V && ((uintptr_t)b & 3) == 0) {
+            // one vector more, from the 16 bytes that b lies in: all lanes lie alike, and single loads took half the kernel's time
+            const int shift = (int)((uintptr_t)b >> 2 & 3);
+            float w[G + 4];
 #pragma unroll
-            for (int i = 0; i < G; ++i) x[i] += __ldg(b + i);
+            for (int i = 0; i < G + 4; i += 4) {
+                const float4 q = __ldg(reinterpret_cast<const float4*>(b - shift + i));
+                w[i] = q.x, w[i + 1] = q.y, w[i + 2] = q.z, w[i + 3] = q.w;
+            }
+#pragma unroll
+            for (int i = 0; i < G; ++i) x[i] += shift == 1 ? w[i + 1] : shift == 2 ? w[i + 2] : w[i + 3];
         } else {
 #pragma unroll
             for (int i = 0; i < G; ++i)
@@ -145,7 +153,7 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
             for (int i = 0; i < 8; ++i) t[i] = i0 + i * AD_THREADS < len ? tok[i0 + i * AD_THREADS] : -1;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (t[i] >= v0 && t[i] < v0 + n) Counts<C>::add(table, P + t[i] - v0);
+                if ((uint32_t)t[i] - (uint32_t)v0 < (uint32_t)n) Counts<C>::add(table, P + t[i] - v0);
         }
         __syncthreads();
         counts = table;

@@ -4,13 +4,14 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <new>
 #include <type_traits>
 #include <vector>
 
 #include <sched.h>
 
 #include "../../include/hbsjd.h"
-#include "internal.h"
+#include "logit_rows.cuh"
 
 using namespace hbsjd;
 
@@ -1125,6 +1126,62 @@ int hbsjd_bikl(hbsjd_ctx* c, const float* logits_s, const float* logits_t, int r
 
 namespace {
 
+// State of a context whose inputs are all tokens of the finished trajectories.  pos: see launch_score_init.
+void score_begin(hbsjd_ctx* x, int batch, const int32_t* tokens, const int32_t* prefix_len, const int32_t* class_labels, float* pos) {
+    State& st = x->st;
+    st.B = batch;
+    st.T = x->T;
+    st.V = x->d.vocab;
+    st.D = x->d.dim;
+    st.Hh = x->d.n_heads;
+    st.dh = x->dh;
+    st.F = x->d.ffn_hidden;
+    st.L = x->d.n_layers;
+    st.C = x->d.n_classes;
+    st.Bmax = x->Bmax;
+    st.Wmax = x->Wmax;
+    st.H = 1;
+    st.nb = 1;
+    x->have_rollout = false;
+    x->live = 0;
+    launch_score_init(st, tokens, class_labels, prefix_len, pos, x->stream);
+    x->launches++;
+}
+
+// One forward of such a context, up to the operand of the head.
+int score_forward(hbsjd_ctx* x, const PassShape& sh) {
+    x->st.W = sh.width;
+    x->st.R = sh.rows;
+    x->st.multi = sh.span > sh.width;
+    launch_setup(x->st, 1, 1, x->stream, sh.span);
+    x->launches++;
+    const int rc = forward_any(x, sh.slots, HEAD_OPERAND);
+    if (rc) return rc;
+    return x->profiling ? sync_counters(x) : 0;  // (folds this forward's event pairs while its byte counters are current)
+}
+
+// The integer inputs of a call on trajectories, checked on the host before any kernel runs.
+int check_trajectories(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32_t* prefix_len, const int32_t* class_labels) {
+    const int T = c->T, V = c->d.vocab;
+    std::vector<int32_t> hk(batch), hl(batch), ht((size_t)batch * T);
+    CK(cudaMemcpyAsync(hk.data(), prefix_len, batch * sizeof(int32_t), cudaMemcpyDeviceToHost, c->stream));
+    CK(cudaMemcpyAsync(hl.data(), class_labels, batch * sizeof(int32_t), cudaMemcpyDeviceToHost, c->stream));
+    CK(cudaMemcpyAsync(ht.data(), tokens, (size_t)batch * T * sizeof(int32_t), cudaMemcpyDeviceToHost, c->stream));
+    CK(cudaStreamSynchronize(c->stream));
+    for (int b = 0; b < batch; ++b) {
+        if (hk[b] < 0 || hk[b] > T || hl[b] < 0 || hl[b] > c->d.n_classes) {
+            snprintf(c->err, sizeof(c->err), "image %d: prefix_len %d or label %d out of range", b, hk[b], hl[b]);
+            return HBSJD_EINVAL;
+        }
+        for (int t = 0; t < T; ++t)
+            if (ht[(size_t)b * T + t] < 0 || ht[(size_t)b * T + t] >= V) {
+                snprintf(c->err, sizeof(c->err), "image %d: token %d out of range", b, t);
+                return HBSJD_EINVAL;
+            }
+    }
+    return HBSJD_OK;
+}
+
 // The forwards of both models and the divergence, on the contexts' streams.
 int score_run(hbsjd_ctx* student, hbsjd_ctx* teacher, int batch, const int32_t* tokens, const int32_t* prefix_len,
               const int32_t* class_labels, float* bikl_pos, float* per_image, float* loss) {
@@ -1134,43 +1191,15 @@ int score_run(hbsjd_ctx* student, hbsjd_ctx* teacher, int batch, const int32_t* 
     float* pos = bikl_pos ? bikl_pos : c->score_pos;
     float* img = per_image ? per_image : c->score_img;
     hbsjd_ctx* both[2] = {student, teacher};
-    for (hbsjd_ctx* x : both) {
-        State& st = x->st;
-        st.B = batch;
-        st.T = T;
-        st.V = V;
-        st.D = x->d.dim;
-        st.Hh = x->d.n_heads;
-        st.dh = x->dh;
-        st.F = x->d.ffn_hidden;
-        st.L = x->d.n_layers;
-        st.C = x->d.n_classes;
-        st.Bmax = x->Bmax;
-        st.Wmax = x->Wmax;
-        st.H = 1;
-        st.nb = 1;
-        x->have_rollout = false;
-        x->live = 0;
-        launch_score_init(st, tokens, class_labels, prefix_len, x == student ? pos : nullptr, x->stream);
-        x->launches++;
-    }
+    for (hbsjd_ctx* x : both) score_begin(x, batch, tokens, prefix_len, class_labels, x == student ? pos : nullptr);
     for (int done = 0, span; done < T; done += span) {
         const PassShape sh = pass_shape(len, done, T, std::min(c->rows_cap, teacher->rows_cap));
         span = sh.span;
         for (hbsjd_ctx* x : both) {
-            x->st.W = sh.width;
-            x->st.R = sh.rows;
-            x->st.multi = span > sh.width;
-            launch_setup(x->st, 1, 1, x->stream, span);
-            x->launches++;
-            const int rc = forward_any(x, sh.slots, HEAD_OPERAND);
+            const int rc = score_forward(x, sh);
             if (rc) {
                 if (x != c) snprintf(c->err, sizeof(c->err), "teacher forward: %.200s", x->err);
                 return rc;
-            }
-            if (x->profiling) {  // fold this forward's event pairs while its byte counters are current
-                const int rs = sync_counters(x);
-                if (rs) return rs;
             }
         }
         // logits and divergence in as few parts of equal size as both contexts have room for
@@ -1219,6 +1248,58 @@ int score_run(hbsjd_ctx* student, hbsjd_ctx* teacher, int batch, const int32_t* 
     return HBSJD_OK;
 }
 
+// The forwards of one model, and the lists of its distributions.
+int score_topk(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32_t* prefix_len, const int32_t* class_labels, int k,
+               float temperature, float* values, int32_t* indices, float* rest) {
+    const int T = c->T, V = c->d.vocab;
+    if (!tokens || !prefix_len || !class_labels || !values || !indices || batch < 1 || batch > c->Bmax || k < 1 || k > MAX_LISTED ||
+        k > V || !(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) {
+        snprintf(c->err, sizeof(c->err), "hbsjd_score_topk: null argument, or batch %d, k %d or temperature %g out of range", batch, k,
+                 temperature);
+        return HBSJD_EINVAL;
+    }
+    if (const int rc = check_trajectories(c, batch, tokens, prefix_len, class_labels)) return rc;
+    const std::vector<int32_t> len(batch, T);  // every token of the sequences is an input
+    score_begin(c, batch, tokens, prefix_len, class_labels, nullptr);
+    TopkArgs a = {};
+    a.x = c->activations;
+    a.ld = V;
+    a.values = values;
+    a.indices = indices;
+    a.rest = rest;
+    a.V = V;
+    a.k = k;
+    a.temperature = temperature;
+    a.prefix_len = prefix_len;
+    a.T = T;
+    CK(launch_topk_clear(a, batch, c->stream));
+    c->launches++;
+    for (int done = 0, span; done < T; done += span) {
+        const PassShape sh = pass_shape(len, done, T, c->rows_cap);
+        span = sh.span;
+        if (const int rc = score_forward(c, sh)) return rc;
+        // logits and lists in as few parts of equal size as there is room for
+        const int parts = (sh.rows + c->score_rows - 1) / c->score_rows;
+        const int step = std::min(c->score_rows, ((sh.rows + parts - 1) / parts + 127) / 128 * 128);
+        for (int row0 = 0; row0 < sh.rows; row0 += step) {
+            const int rows = std::min(step, sh.rows - row0);
+            float* out = (float*)c->activations;
+            const int rc = c->bf16_model ? head<bf16>(c, row0, rows, out, c->score_rows) : head<float>(c, row0, rows, out, c->score_rows);
+            if (rc) return rc;
+            a.at = c->st.row_pos + row0;
+            // timed with the vocabulary-wide class: V floats read per input
+            const int ps = prof_begin(c, HBSJD_PROF_ACCEPT, 4.0 * rows * V);
+            CK(launch_topk(a, rows, HBSJD_DTYPE_FP32, c->stream));
+            prof_end(c, ps);
+            c->launches++;
+        }
+        launch_prefill_advance(c->st, span, c->stream);
+        c->launches++;
+    }
+    CK(cudaGetLastError());
+    return sync_counters(c);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1239,23 +1320,7 @@ int hbsjd_score(hbsjd_ctx* student, hbsjd_ctx* teacher, int batch, const int32_t
                  batch);
         return HBSJD_EINVAL;
     }
-    // validate the integer inputs on the host before any kernel runs
-    std::vector<int32_t> hk(batch), hl(batch), ht((size_t)batch * T);
-    CK(cudaMemcpyAsync(hk.data(), prefix_len, batch * sizeof(int32_t), cudaMemcpyDeviceToHost, c->stream));
-    CK(cudaMemcpyAsync(hl.data(), class_labels, batch * sizeof(int32_t), cudaMemcpyDeviceToHost, c->stream));
-    CK(cudaMemcpyAsync(ht.data(), tokens, (size_t)batch * T * sizeof(int32_t), cudaMemcpyDeviceToHost, c->stream));
-    CK(cudaStreamSynchronize(c->stream));
-    for (int b = 0; b < batch; ++b) {
-        if (hk[b] < 0 || hk[b] > T || hl[b] < 0 || hl[b] > c->d.n_classes) {
-            snprintf(c->err, sizeof(c->err), "image %d: prefix_len %d or label %d out of range", b, hk[b], hl[b]);
-            return HBSJD_EINVAL;
-        }
-        for (int t = 0; t < T; ++t)
-            if (ht[(size_t)b * T + t] < 0 || ht[(size_t)b * T + t] >= V) {
-                snprintf(c->err, sizeof(c->err), "image %d: token %d out of range", b, t);
-                return HBSJD_EINVAL;
-            }
-    }
+    if (const int rc = check_trajectories(c, batch, tokens, prefix_len, class_labels)) return rc;
     // The two models are independent until their logits meet.  Contexts that share a stream would run one after the
     // other, and most of a forward of few images is latency (every forward has tails in which SMs idle), so the student
     // moves to a stream of its own for the call, behind everything the shared stream holds, and back: 9 images of B
@@ -1278,6 +1343,18 @@ int hbsjd_score(hbsjd_ctx* student, hbsjd_ctx* teacher, int batch, const int32_t
         }
     }
     return rc;
+}
+
+int hbsjd_score_topk(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32_t* prefix_len, const int32_t* class_labels, int k,
+                     float temperature, float* values, int32_t* indices, float* rest) {
+    if (!c) return HBSJD_EINVAL;
+    c->err[0] = 0;
+    try {
+        return score_topk(c, batch, tokens, prefix_len, class_labels, k, temperature, values, indices, rest);
+    } catch (const std::bad_alloc&) {
+        snprintf(c->err, sizeof(c->err), "hbsjd_score_topk: out of host memory");
+        return HBSJD_ENOMEM;
+    }
 }
 
 int hbsjd_profile(hbsjd_ctx* c, int enable) {

@@ -509,6 +509,8 @@ struct TopkArgs {
     int T;
 };
 cudaError_t launch_topk(const TopkArgs& a, int rows, int dtype, Stream& s);
+// empty lists for the positions of the images' prefixes (a.prefix_len, a.T)
+cudaError_t launch_topk_clear(const TopkArgs& a, int batch, Stream& s);
 
 struct AdjustArgs {
     const void *x, *u;

@@ -511,6 +511,19 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
     }
 }
 
+// One CTA per image: empty lists for its prefix.
+__global__ void k_topk_clear(TopkArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int64_t first = (int64_t)blockIdx.x * a.T;
+    const int len = min(a.prefix_len[blockIdx.x], a.T);
+    for (int64_t i = threadIdx.x; i < (int64_t)len * a.k; i += blockDim.x) {
+        a.values[first * a.k + i] = -INFINITY;
+        a.indices[first * a.k + i] = -1;
+    }
+    for (int i = threadIdx.x; i < len && a.rest; i += blockDim.x) a.rest[first + i] = -INFINITY;
+}
+
 template <typename T>
 cudaError_t run_topk(TopkArgs& a, Stream& s) {
     constexpr int G = 16 / sizeof(T);
@@ -536,6 +549,10 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
 }
 
 }  // namespace
+
+cudaError_t launch_topk_clear(const TopkArgs& a, int batch, Stream& s) {
+    return launch_k(k_topk_clear, dim3(batch), dim3(512), 0, s, a);
+}
 
 cudaError_t launch_topk(const TopkArgs& args, int rows, int dtype, Stream& s) {
     TopkArgs a = args;
