@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     constexpr int G = 16 / sizeof(TS), WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ ListCoefs coefs;
-    __shared__ int repeated[3];
+    __shared__ int repeated[2];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, k = a.k;
@@ -242,16 +242,16 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     const int step = gridDim.x / a.ctas, places = WARPS * a.ctas;
     const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
     TS* ss = (TS*)smem;
-    // Two or three of each, by turns: a CTA may be a row ahead of others, and a warp, and lists are made a row ahead.
+    // Two of each, by turns: a CTA may be a row ahead of others, and a warp, and lists are made a row ahead.
     const int words = (a.slice + 31) / 32;
     Pair* slots = (Pair*)(ss + a.slice + 16);         // [2][places]
     Mass* slots_other = (Mass*)(slots + 2 * places);  // [2][places]
-    float* xks = (float*)(slots_other + 2 * places);  // [3][k] the student's logit of a listed token of the slice
-    float* vals = xks + 3 * k;                        // [3][k] the teacher's
-    int32_t* ats = (int32_t*)(vals + 3 * k);          // [3][k] its place in the slice, -1: not here, or listed before
-    uint32_t* seen = (uint32_t*)(ats + 3 * k);        // [2][words] a bit per element of the slice, 0 between lists
-    for (int i = threadIdx.x; i < 2 * words; i += THREADS) seen[i] = 0;
-    if (threadIdx.x < 3) repeated[threadIdx.x] = 0;
+    float* xks = (float*)(slots_other + 2 * places);  // [2][k] the student's logit of a listed token of the slice
+    float* vals = xks + 2 * k;                        // [2][k] the teacher's
+    int32_t* ats = (int32_t*)(vals + 2 * k);          // [2][k] its place in the slice, -1: not here, or listed before
+    uint32_t* seen = (uint32_t*)(ats + 2 * k);        // [words] a bit per element of the slice, 0 between lists
+    for (int i = threadIdx.x; i < words; i += THREADS) seen[i] = 0;
+    if (threadIdx.x < 2) repeated[threadIdx.x] = 0;
     __syncthreads();
     if (a.ctas > 1) {
         cluster_arrive();
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     };
     // A row's list, one entry a thread (the last warps first: warp 0 has other work): those of the slice find their places.
     const int first = THREADS - 1 - threadIdx.x;
-    const auto list = [&](int row, int turn, int odd, int32_t token, float value) {
+    const auto list = [&](int row, int turn, int32_t token, float value) {
         for (int i = first; i < k; i += THREADS) {
             if (i >= THREADS) {
                 token = __ldg(a.indices + (int64_t)row * k + i);
@@ -273,23 +273,22 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
             int e = -1;
             if (token >= v0 && token < v0 + n && !(value == -INFINITY)) {
                 e = token - v0;
-                if (atomicOr(&seen[odd * words + (e >> 5)], 1u << (e & 31)) >> (e & 31) & 1) repeated[turn] = 1;
+                if (atomicOr(&seen[e >> 5], 1u << (e & 31)) >> (e & 31) & 1) repeated[turn] = 1;
             }
             ats[turn * k + i] = e;
             vals[turn * k + i] = value;
         }
     };
-    int row = blockIdx.x / a.ctas, parity = 0, turn = 0, odd = 0;
+    int row = blockIdx.x / a.ctas, parity = 0, turn = 0;
     float w = weight(row), w1 = weight(row + step);
     if (w != 0.f) {
         fetch(row);
-        if (first < k) list(row, 0, 0, __ldg(a.indices + (int64_t)row * k + first), __ldg(a.values + (int64_t)row * k + first));
+        if (first < k) list(row, 0, __ldg(a.indices + (int64_t)row * k + first), __ldg(a.values + (int64_t)row * k + first));
     }
     __syncthreads();
-    for (; row < a.rows; row += step, odd ^= 1) {
+    for (; row < a.rows; row += step, turn ^= 1) {
         const float w2 = weight(row + 2 * step);  // (so that no fetch waits for a weight)
         bool fetched = w1 == 0.f;
-        const int turn1 = turn == 2 ? 0 : turn + 1;
         int32_t token = -1;
         float value = 0.f;
         if (w1 != 0.f && first < k) {
@@ -302,18 +301,19 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
         if (w == 0.f) {                                       // (all CTAs of the row)
             if (g) put_zeros(g, lo, hi);
             if (a.loss && rank == 0 && threadIdx.x == 0) a.loss[row] = 0.f;
-            if (threadIdx.x == 0) repeated[3 - turn - turn1] = 0;
-            if (w1 != 0.f) list(row + step, turn1, odd ^ 1, token, value);
+            if (threadIdx.x == 0) repeated[turn ^ 1] = 0;
+            __syncthreads();  // the row before is done with the other list
+            if (w1 != 0.f) list(row + step, turn ^ 1, token, value);
             __syncthreads();
         } else {
             const float yr = a.rest ? __ldg(a.rest + row) : -INFINITY;
             float* xk = xks + turn * k;
             const float* val = vals + turn * k;
             int32_t* at = ats + turn * k;
-            // (the third turn's was read before the others were last met; those who set it will meet this thread first)
-            if (threadIdx.x == 0) repeated[3 - turn - turn1] = 0;
+            // (the row before has read its own; those who set it again will meet this thread first)
+            if (threadIdx.x == 0) repeated[turn ^ 1] = 0;
             for (int i = first; i < k; i += THREADS)
-                if (at[i] >= 0) seen[odd * words + (at[i] >> 5)] = 0;
+                if (at[i] >= 0) seen[at[i] >> 5] = 0;
             if (repeated[turn]) {  // of a token that is listed twice, the first entry counts
                 for (int i0 = 0; i0 < k; i0 += THREADS) {
                     const int i = i0 + threadIdx.x;
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                     }
                 }
             }
-            if (w1 != 0.f) list(row + step, turn1, odd ^ 1, token, value);
+            if (w1 != 0.f) list(row + step, turn ^ 1, token, value);  // (the one before is used up; the others wait for one warp)
             __syncthreads();
             if (g) {
                 const ListCoefs f = coefs;
@@ -481,7 +481,6 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
             }
             parity ^= 1;
         }
-        turn = turn1;
         __syncwarp();  // the warp's part is done
         if (!fetched) fetch(row + step);
         w = w1, w1 = w2;
@@ -525,8 +524,8 @@ template <typename TS>
 cudaError_t run_distill_topk(const DistillArgs& a, Stream& s) {
     return by_threads(a, 16 / sizeof(TS), 16, [&](auto threads) {
         constexpr int THREADS = decltype(threads)::value, PER_SM = 1536 / THREADS;
-        const size_t smem = (a.slice + 16) * sizeof(TS) + 2 * THREADS / 32 * a.ctas * (sizeof(Pair) + sizeof(Mass)) + a.k * 36 +
-                            (a.slice + 31) / 32 * 8;
+        const size_t smem = (a.slice + 16) * sizeof(TS) + 2 * THREADS / 32 * a.ctas * (sizeof(Pair) + sizeof(Mass)) + a.k * 24 +
+                            (a.slice + 31) / 32 * 4;
         int clusters = 0;
         const cudaError_t e = deal<k_distill_topk<TS, THREADS, PER_SM>, THREADS, PER_SM>(a, smem, &clusters);
         if (e != cudaSuccess) return e;
