@@ -511,7 +511,7 @@ template <typename TS, typename TT>
 cudaError_t run_distill(const DistillArgs& a, Stream& s) {
     constexpr int G = sizeof(TS) == 2 && sizeof(TT) == 2 ? 8 : 4;
     return by_threads(a, G, 8, [&](auto threads) {
-        constexpr int THREADS = decltype(threads)::value, PER_SM = 1024 / THREADS;
+        constexpr int THREADS = decltype(threads)::value, PER_SM = THREADS == 512 ? 2 : 768 / THREADS;  // (80 registers where there is room for three)
         const size_t smem = (a.slice + 16) * (sizeof(TS) + sizeof(TT)) + 2 * THREADS / 32 * a.ctas * sizeof(Pair);
         int clusters = 0;
         const cudaError_t e = deal<k_distill<TS, TT, THREADS, PER_SM>, THREADS, PER_SM>(a, smem, &clusters);
