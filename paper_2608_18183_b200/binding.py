@@ -276,7 +276,7 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
         if not sequences or not cap:
             tok = None
     if out is None:
-        out = logits.new_empty(shape)
+        out = _torch.empty_like(logits, memory_format=_torch.contiguous_format)
     o, ld_out, _ = _rows(what, "out", out, device, logits.dtype, shape, written=True)
     if rows == 0:
         return out
@@ -317,7 +317,7 @@ def _distill(what, entry, logits_s, s, ld_s, dtype_s, teacher, dtype_t, ld_t, k,
     if grad is not None:
         g, ld_g, _ = _rows(what, "grad", grad, device, logits_s.dtype, shape, written=True)
     elif want_grad:
-        grad = logits_s.new_empty(shape)
+        grad = _torch.empty_like(logits_s, memory_format=_torch.contiguous_format)
         g, ld_g = grad.data_ptr(), V
     else:
         g, ld_g = None, 0

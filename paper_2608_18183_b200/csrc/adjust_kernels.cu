@@ -13,7 +13,6 @@ namespace hbsjd {
 
 namespace {
 
-constexpr int AD_THREADS = 256;
 constexpr int AD_AHEAD = 2;  // groups of 16 bytes that a thread has on their way
 
 // How often the tokens of a chunk occur, in shared memory: 16 bits each where no history is longer than they count to.
@@ -110,8 +109,8 @@ __device__ __forceinline__ void apply_rules(const AdjustArgs& a, const uint32_t*
     for (int i = 0; i < G; ++i) x[i] = fmaxf(x[i], -INFINITY);  // (of NaN and a number, the number)
 }
 
-template <typename T, bool GUIDED, typename C>
-__global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, int chunks) {
+template <typename T, bool GUIDED, typename C, int THREADS>
+__global__ void __launch_bounds__(THREADS) k_adjust(AdjustArgs a, int chunk, int chunks) {
     constexpr int G = 16 / sizeof(T);
     extern __shared__ __align__(16) unsigned char smem[];
     pdl_wait();
@@ -128,7 +127,7 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
     T* out = (T*)a.out + row * a.ld_out + v0;
     // groups of 16 bytes of the output: the entry of a thread's first, and the entries from one to its next
     const int P = phase_of(out), e0 = tid * G - P;
-    constexpr int STEP = AD_THREADS * G;
+    constexpr int STEP = THREADS * G;
     const bool wide = phase_of(x) == P && (!GUIDED || phase_of(u) == P);
     uint4 f[AD_AHEAD], g[AD_AHEAD];
     const auto load = [&](int slot, int e) {
@@ -144,13 +143,13 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
     if (h < 0 || h >= a.histories) len = 0;
     if (len > 0) {
         uint32_t* table = (uint32_t*)smem;  // element P is the chunk's first
-        for (int i = tid * 16; i < (P + n + G) * (int)sizeof(C); i += AD_THREADS * 16) *reinterpret_cast<uint4*>(smem + i) = make_uint4(0, 0, 0, 0);
+        for (int i = tid * 16; i < (P + n + G) * (int)sizeof(C); i += THREADS * 16) *reinterpret_cast<uint4*>(smem + i) = make_uint4(0, 0, 0, 0);
         __syncthreads();
         const int32_t* tok = a.history + h * a.ld_history;
-        for (int i0 = tid; i0 < len; i0 += AD_THREADS * 8) {
+        for (int i0 = tid; i0 < len; i0 += THREADS * 8) {
             int32_t t[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = i0 + i * AD_THREADS < len ? tok[i0 + i * AD_THREADS] : -1;
+            for (int i = 0; i < 8; ++i) t[i] = i0 + i * THREADS < len ? tok[i0 + i * THREADS] : -1;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if ((uint32_t)t[i] - (uint32_t)v0 < (uint32_t)n) Counts<C>::add(table, P + t[i] - v0);
@@ -189,19 +188,28 @@ __global__ void __launch_bounds__(AD_THREADS) k_adjust(AdjustArgs a, int chunk, 
     }
 }
 
-template <typename T, bool GUIDED, typename C>
+template <typename T, bool GUIDED, typename C, int THREADS>
 cudaError_t run_adjust(const AdjustArgs& a, int rows, Stream& s) {
     constexpr int G = 16 / sizeof(T);
-    const cudaError_t e = allow_row_smem<k_adjust<T, GUIDED, C>>();
+    const cudaError_t e = allow_row_smem<k_adjust<T, GUIDED, C, THREADS>>();
     if (e != cudaSuccess) return e;
     // Every chunk reads the row's whole history, and its table takes shared memory: 4096 guided rows of 16384 fp32 with histories of 256
     // take 138, 131 and 162 us with chunks of 4096, 8192 and 16384 entries, 771 rows of 50021 bf16 with histories of up to 4096
     // 77, 63 and 68.  Smaller chunks where rows are few.
-    int chunk = 8192;
-    while (chunk > AD_THREADS * G && (int64_t)rows * ((a.V + chunk - 1) / chunk) < 2 * device_sm_count()) chunk /= 2;
+    int chunk = 32 * THREADS;
+    while (chunk > THREADS * G && (int64_t)rows * ((a.V + chunk - 1) / chunk) < 2 * device_sm_count()) chunk /= 2;
     const int chunks = (a.V + chunk - 1) / chunk;
     const size_t smem = a.history ? ((size_t)std::min(chunk, a.V) + 32) * sizeof(C) : 0;
-    return launch_k(k_adjust<T, GUIDED, C>, dim3((unsigned)rows * chunks), dim3(AD_THREADS), smem, s, a, chunk, chunks);
+    return launch_k(k_adjust<T, GUIDED, C, THREADS>, dim3((unsigned)rows * chunks), dim3(THREADS), smem, s, a, chunk, chunks);
+}
+
+template <typename T, bool GUIDED, typename C>
+cudaError_t run_adjust(const AdjustArgs& a, int rows, Stream& s) {
+    // Rows of one chunk: threads that have several groups each (16384 rows of 1000 fp32: 31 us with 64 threads, 52 with 256; of 3001:
+    // 85 us with 128, 95 with 256).
+    if (a.V <= 2048) return run_adjust<T, GUIDED, C, 64>(a, rows, s);
+    if (a.V <= 4096) return run_adjust<T, GUIDED, C, 128>(a, rows, s);
+    return run_adjust<T, GUIDED, C, 256>(a, rows, s);
 }
 
 template <typename T>

@@ -487,12 +487,14 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     }
 }
 
-// Threads of a CTA: 128 to 512, with at least `least` groups each if there are many rows.  What a warp does once a row is a good
+// Threads of a CTA: 32 to 512, with at least `least` groups each if there are many rows.  What a warp does once a row is a good
 // part of its work, so that fewer warps are faster (16384 rows of 16384 fp32, lists of 64: 395 us with 256 threads, 439 with 512)
 // as long as other CTAs fill the SM; few rows have the SMs to themselves.
 template <typename F>
 cudaError_t by_threads(const DistillArgs& a, int G, int least, F&& f) {
     const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? least : 4) * G;
+    if (a.slice <= 32 * per) return f(std::integral_constant<int, 32>());
+    if (a.slice <= 64 * per) return f(std::integral_constant<int, 64>());
     if (a.slice <= 128 * per) return f(std::integral_constant<int, 128>());
     if (a.slice <= 256 * per) return f(std::integral_constant<int, 256>());
     return f(std::integral_constant<int, 512>());
@@ -523,7 +525,7 @@ cudaError_t run_distill(const DistillArgs& a, Stream& s) {
 template <typename TS>
 cudaError_t run_distill_topk(const DistillArgs& a, Stream& s) {
     return by_threads(a, 16 / sizeof(TS), 16, [&](auto threads) {
-        constexpr int THREADS = decltype(threads)::value, PER_SM = 1536 / THREADS;
+        constexpr int THREADS = decltype(threads)::value, PER_SM = std::min(32, 1536 / THREADS);
         const size_t smem = (a.slice + 16) * sizeof(TS) + 2 * THREADS / 32 * a.ctas * (sizeof(Pair) + sizeof(Mass)) + a.k * 24 +
                             (a.slice + 31) / 32 * 4;
         int clusters = 0;

@@ -447,22 +447,32 @@ template <auto Kernel>
 inline cudaError_t resident_clusters(int ctas, int threads, int per_sm, size_t smem, int64_t rows, int* clusters) {
     const int sms = device_sm_count();
     *clusters = (int)std::min<int64_t>(rows, std::max(1, sms * per_sm / ctas));
-    if (ctas <= 2 || rows * ctas <= sms / 2) return cudaSuccess;
-    // larger clusters lie within groups of SMs that they may not fill
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(sms * per_sm / ctas * ctas);
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = ctas;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    int most = 0;
-    const cudaError_t e = cudaOccupancyMaxActiveClusters(&most, Kernel, &cfg);
-    if (e == cudaSuccess && most > 0) *clusters = std::min(*clusters, most);
-    return e;
+    if (ctas <= 2 || rows * ctas * 2 <= (int64_t)sms * per_sm) return cudaSuccess;
+    // Larger clusters lie within groups of SMs that they may not fill.  The last answer is kept: a loop asks for one shape.
+    static std::atomic<uint64_t> last{0};  // device, shared memory, CTAs; then the answer
+    int dev = 0, most = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t asked = (((uint64_t)(dev + 1) << 24 | smem) << 4 | (uint64_t)ctas) << 16, known = last.load(std::memory_order_relaxed);
+    if ((known & ~(uint64_t)0xffff) == asked) {
+        most = (int)(known & 0xffff);
+    } else {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(sms * per_sm / ctas * ctas);
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = ctas;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        e = cudaOccupancyMaxActiveClusters(&most, Kernel, &cfg);
+        if (e != cudaSuccess) return e;
+        last.store(asked | (uint64_t)std::min(most, 0xffff), std::memory_order_relaxed);
+    }
+    if (most > 0) *clusters = std::min(*clusters, most);
+    return cudaSuccess;
 }
 
 // How a row is split: CTAs (a cluster, where more than one) and the elements that each holds.

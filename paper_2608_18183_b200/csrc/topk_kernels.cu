@@ -84,8 +84,15 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
     }
 }
 
+// CTAs of an SM, at most: three of 256 threads, which is what rows of 16384 fp32 leave room for, with the registers that they may
+// have then (lists of 64 from 8192 such rows: 138 us, with 40 registers 148).
+template <int THREADS>
+constexpr int topk_ctas() {
+    return THREADS == 256 ? 3 : 1536 / THREADS;
+}
+
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) k_topk(TopkArgs a) {
+__global__ void __launch_bounds__(THREADS, topk_ctas<THREADS>()) k_topk(TopkArgs a) {
     constexpr int G = 16 / sizeof(T), WARPS = THREADS / 32, SETS = 4;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ Mass rests[ROW_CTAS];  // of the slices
@@ -534,7 +541,7 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
         constexpr int THREADS = decltype(threads)::value;
         cudaError_t e = allow_row_smem<k_topk<T, THREADS>>();
         if (e != cudaSuccess) return e;
-        const int per_sm = std::max(1, std::min<int>(1536 / THREADS, 227 * 1024 / (smem + 1024 + 1600)));  // (1 KB is the system's)
+        const int per_sm = std::max(1, std::min<int>(topk_ctas<THREADS>(), 227 * 1024 / (smem + 1024 + 1600)));  // (1 KB is the system's)
         int clusters = 0;
         e = resident_clusters<k_topk<T, THREADS>>(a.ctas, THREADS, per_sm, smem, a.rows, &clusters);
         if (e != cudaSuccess) return e;
@@ -543,6 +550,7 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
     // Sixteen groups a thread at least, as for the divergences (lists of 64 from 8192 rows of 16384 fp32: 148 us with 256 threads, 185
     // with 512), four where there are few rows; and two maxima per entry of the list.
     const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? 16 : 4) * G;
+    if (a.slice <= 64 * per && a.k <= 128) return run(std::integral_constant<int, 64>());
     if (a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
     if (a.slice <= 256 * per && a.k <= 512) return run(std::integral_constant<int, 256>());
     return run(std::integral_constant<int, 512>());
