@@ -277,7 +277,9 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
             tok = None
     if out is None:
         out = _torch.empty_like(logits, memory_format=_torch.contiguous_format)
-    o, ld_out, _ = _rows(what, "out", out, device, logits.dtype, shape, written=True)
+        o, ld_out = out.data_ptr(), V
+    else:
+        o, ld_out, _ = _rows(what, "out", out, device, logits.dtype, shape, written=True)
     if rows == 0:
         return out
     d = hbsjd_adjust_desc(rows, V, dtype, masks, sequences, cap, ld, ld_u, ld_out, ld_mask, ld_history, cfg_scale, repetition,

@@ -334,14 +334,16 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
             end_part(ss, p, PAD);
             // they leave the row; v: their sums, student and teacher
             Pair v = Pair::none();
+            bool any = false;
             each([&](int i, int e) {
+                any = true;
                 const float x = to_f<TS>(ss[e]);
                 xk[i] = x;
                 ss[e] = from_f<TS>(-INFINITY);
                 v.ms = fmaxf(v.ms, x);
                 v.mt = fmaxf(v.mt, val[i]);
             });
-            if (__any_sync(0xffffffffu, v.mt > -INFINITY || v.ms > -INFINITY)) {
+            if (__any_sync(0xffffffffu, any)) {
                 v.share();
                 const float os = v.ms == -INFINITY ? 0.f : v.ms, ot = v.mt == -INFINITY ? 0.f : v.mt;
                 each([&](int i, int) {

@@ -416,8 +416,8 @@ __global__ void __launch_bounds__(THREADS, topk_ctas<THREADS>()) k_topk(TopkArgs
                 for (int j = first; j < last; ++j) r += other[j] > key;
                 cand[r] = key;
             }
-            __syncthreads();
         }
+        __syncthreads();  // (with one candidate, too: what is reset below was read)
         const unsigned long long* sorted = cand;
         if (tid == 0) {
             found = bad = big = 0;

@@ -523,6 +523,33 @@ def test_distill_topk_masks_infinities_and_nan():
                 assert loss[8] == float("inf") and bool(((grad[8][at].double() - want).abs() < 3e-5).all())
 
 
+def test_a_teacher_s_nan_shows_wherever_it_stands():
+    """NaN among the listed values, also alone in its part of the row and where the student has no mass."""
+    import torch
+    for V, rows in ((700, 40), (16384, 200)):
+        s = _rows(1, rows, V)
+        values = torch.randn(rows, 12, generator=_gen(2), device="cuda")
+        indices = torch.stack([torch.randperm(V, generator=_gen(3 + r), device="cuda")[:12] for r in range(rows)]).int()
+        rest = torch.zeros(rows, device="cuda")
+        clean = binding.hbsjd_distill_topk(s, values, indices, rest, forward=0.5, reverse=0.5)
+        values[::2, 5] = float("nan")
+        s[::2].scatter_(1, indices[::2, 5:6].long(), NEG)
+        loss, grad = binding.hbsjd_distill_topk(s, values, indices, rest, forward=0.5, reverse=0.5)
+        assert bool(torch.isnan(loss[::2]).all()) and bool(torch.isnan(grad[::2]).all())
+        assert torch.equal(loss[1::2], clean[0][1::2]) and torch.equal(grad[1::2], clean[1][1::2])
+
+
+def test_lists_of_one_again_and_again():
+    """k = 1 leaves the selection one candidate; thousands of such rows per CTA, in rows of one CTA and of several."""
+    import torch
+    for V, rows in ((40, 9000), (1200, 9000), (5000, 6000), (90000, 300)):
+        x = _rows(V, rows, V)
+        for _ in range(3):
+            values, indices, rest = binding.hbsjd_topk_logits(x, 1)
+            m = x.max(-1)
+            assert torch.equal(values[:, 0], m.values) and torch.equal(indices[:, 0].long(), m.indices)
+
+
 def test_a_list_of_everything_is_the_whole_divergence():
     import torch
     s, t = _rows(1, 9, 1000), _rows(2, 9, 1000)
