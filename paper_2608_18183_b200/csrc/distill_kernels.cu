@@ -514,7 +514,7 @@ cudaError_t deal(const DistillArgs& a, size_t smem, int* clusters) {
 template <typename TS, typename TT>
 cudaError_t run_distill(const DistillArgs& a, Stream& s) {
     constexpr int G = sizeof(TS) == 2 && sizeof(TT) == 2 ? 8 : 4;
-    return by_threads(a, G, 8, [&](auto threads) {
+    return by_threads(a, G, 9, [&](auto threads) {
         constexpr int THREADS = decltype(threads)::value, PER_SM = THREADS == 512 ? 2 : 768 / THREADS;  // (80 registers where there is room for three)
         const size_t smem = (a.slice + 16) * (sizeof(TS) + sizeof(TT)) + 2 * THREADS / 32 * a.ctas * sizeof(Pair);
         int clusters = 0;
@@ -526,7 +526,7 @@ cudaError_t run_distill(const DistillArgs& a, Stream& s) {
 
 template <typename TS>
 cudaError_t run_distill_topk(const DistillArgs& a, Stream& s) {
-    return by_threads(a, 16 / sizeof(TS), 16, [&](auto threads) {
+    return by_threads(a, 16 / sizeof(TS), 18, [&](auto threads) {
         constexpr int THREADS = decltype(threads)::value, PER_SM = std::min(32, 1536 / THREADS);
         const size_t smem = (a.slice + 16) * sizeof(TS) + 2 * THREADS / 32 * a.ctas * (sizeof(Pair) + sizeof(Mass)) + a.k * 24 +
                             (a.slice + 31) / 32 * 4;

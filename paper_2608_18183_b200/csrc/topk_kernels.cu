@@ -547,9 +547,9 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
         if (e != cudaSuccess) return e;
         return launch_kc(true, k_topk<T, THREADS>, dim3((unsigned)clusters * a.ctas), dim3(THREADS), smem, s, a.ctas, a);
     };
-    // Sixteen groups a thread at least, as for the divergences (lists of 64 from 8192 rows of 16384 fp32: 148 us with 256 threads, 185
+    // Eighteen groups a thread (256 threads for the largest slice), as for the divergences (lists of 64 from 8192 rows of 16384 fp32: 148 us with 256 threads, 185
     // with 512), four where there are few rows; and two maxima per entry of the list.
-    const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? 16 : 4) * G;
+    const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? 18 : 4) * G;
     if (a.slice <= 64 * per && a.k <= 128) return run(std::integral_constant<int, 64>());
     if (a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
     if (a.slice <= 256 * per && a.k <= 512) return run(std::integral_constant<int, 256>());
