@@ -136,7 +136,8 @@ __device__ __forceinline__ void stage_row(T* dst, const T* src, int n, int P) {
         // words of the less than VEC elements in front, and of those behind
         const int head_end = min(first * VEC, end), tail = max(last * VEC, head_end), w = P / W + tid;
         if (w * W < head_end) cp_async4(dst + w * W, base + w * W);
-        if (tid >= 32 && tail + (tid - 32) * W < end) cp_async4(dst + tail + (tid - 32) * W, base + tail + (tid - 32) * W);
+        const int q = tid - (THREADS > 32 ? 32 : 16);  // (other threads than those of the head)
+        if (q >= 0 && tail + q * W < end) cp_async4(dst + tail + q * W, base + tail + q * W);
     } else if ((phase_of(src) - P) % W == 0) {
 #pragma unroll 8
         for (int w = P / W + tid; w * W < end; w += THREADS) cp_async4(dst + w * W, base + w * W);

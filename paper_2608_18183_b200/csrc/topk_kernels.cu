@@ -88,7 +88,7 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
 // have then (lists of 64 from 8192 such rows: 138 us, with 40 registers 148).
 template <int THREADS>
 constexpr int topk_ctas() {
-    return THREADS == 256 ? 3 : 1536 / THREADS;
+    return THREADS == 256 ? 3 : THREADS == 32 ? 32 : 1536 / THREADS;
 }
 
 template <typename T, int THREADS>
@@ -550,6 +550,7 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
     // Eighteen groups a thread (256 threads for the largest slice), as for the divergences (lists of 64 from 8192 rows of 16384 fp32: 148 us with 256 threads, 185
     // with 512), four where there are few rows; and two maxima per entry of the list.
     const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? 18 : 4) * G;
+    if (a.slice <= 32 * per && a.k <= 64) return run(std::integral_constant<int, 32>());
     if (a.slice <= 64 * per && a.k <= 128) return run(std::integral_constant<int, 64>());
     if (a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
     if (a.slice <= 256 * per && a.k <= 512) return run(std::integral_constant<int, 256>());
