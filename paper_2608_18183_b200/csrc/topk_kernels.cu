@@ -8,7 +8,7 @@
 // against the bound; the candidates go into bins over their own range, and those of one bin are counted against one another.  No
 // difference of masses is taken: the rest keeps its digits however small it is.  Candidates that do not fit (an order of the row that
 // puts the largest into few threads' entries, ties without end) are narrowed by histograms over the entries themselves.
-// A row is read from HBM once; the barriers between these steps and their latency bound the kernel (three CTAs an SM, 17000 cycles
+// A row is read from HBM once; the barriers between these steps and their latency bound the kernel (three CTAs an SM, 14000 cycles
 // a row of 16384 fp32, of which HBM would need 8500).  The next row is fetched while the list is put in order.  The CTAs of
 // a cluster select from their slices; the first merges the lists.
 #include "logit_rows.cuh"
