@@ -345,6 +345,8 @@ int hbsjd_score(hbsjd_ctx *student, hbsjd_ctx *teacher, int batch, const int32_t
  *   - An array that is written may be one that is read (same pointer, stride and type); else they do not overlap.
  *   - 1 <= V <= 131072, 0 <= rows < 2^27; rows = 0 does nothing.  Element types are HBSJD_DTYPE_*; arithmetic is fp32,
  *     bf16 results are rounded once.
+ *   - A call gives the same bits every time.  The order of a row's sums depends on how the row is aligned and on how many rows
+ *     there are, not on what else is asked for.
  *   - Errors: HBSJD_EINVAL (nothing was launched), HBSJD_ECUDA.  hbsjd_last_error(NULL) tells the calling thread the
  *     details of its last failed one. */
 

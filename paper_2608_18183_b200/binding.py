@@ -303,7 +303,7 @@ def hbsjd_topk_logits(logits, k, temperature=1.0, want_rest=True, stream=None):
     if not 1 <= k <= min(V, 1024):
         _refuse(what, f"k = {k} is out of range")
     values = logits.new_empty((rows, k), dtype=_torch.float32)
-    indices = logits.new_empty((rows, k), dtype=_torch.int32)
+    indices = _torch.empty_like(values, dtype=_torch.int32)
     rest = logits.new_empty((rows,), dtype=_torch.float32) if want_rest else None
     if rows:
         _call(what, load().hbsjd_topk_logits, device, hbsjd_topk_desc(rows, V, dtype, k, ld, temperature, 0), x,

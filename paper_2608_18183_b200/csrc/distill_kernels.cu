@@ -541,7 +541,7 @@ cudaError_t run_distill_topk(const DistillArgs& a, Stream& s) {
 
 cudaError_t launch_distill(const DistillArgs& args, int rows, int dtype_s, int dtype_t, Stream& s) {
     DistillArgs a = args;
-    const RowSplit sp = split_row(rows, a.V, (dtype_s ? 2 : 4) + (dtype_t ? 2 : 4), device_sm_count());
+    const RowSplit sp = split_row(rows, a.V, (dtype_s ? 2 : 4) + (dtype_t ? 2 : 4), device_sm_count(), SHARED_SM, true);
     a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice;
     if (dtype_s) return dtype_t ? run_distill<bf16, bf16>(a, s) : run_distill<bf16, float>(a, s);
     return dtype_t ? run_distill<float, bf16>(a, s) : run_distill<float, float>(a, s);
@@ -549,7 +549,7 @@ cudaError_t launch_distill(const DistillArgs& args, int rows, int dtype_s, int d
 
 cudaError_t launch_distill_topk(const DistillArgs& args, int rows, int dtype_s, Stream& s) {
     DistillArgs a = args;
-    const RowSplit sp = split_row(rows, a.V, dtype_s ? 2 : 4, device_sm_count());
+    const RowSplit sp = split_row(rows, a.V, dtype_s ? 2 : 4, device_sm_count(), SHARED_SM, true);
     a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice;
     return dtype_s ? run_distill_topk<bf16>(a, s) : run_distill_topk<float>(a, s);
 }

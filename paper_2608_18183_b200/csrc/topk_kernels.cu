@@ -84,6 +84,8 @@ __device__ __forceinline__ uint32_t bound_key(uint32_t lo, uint32_t hi, int want
     }
 }
 
+constexpr int ALONE_SM = 160 * 1024;  // (lists and candidates of 1024 need 48 KB beside the row)
+
 // CTAs of an SM, at most: three of 256 threads, which is what rows of 16384 fp32 leave room for, with the registers that they may
 // have then (lists of 64 from 8192 such rows: 138 us, with 40 registers 148).
 template <int THREADS>
@@ -547,12 +549,14 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
         if (e != cudaSuccess) return e;
         return launch_kc(true, k_topk<T, THREADS>, dim3((unsigned)clusters * a.ctas), dim3(THREADS), smem, s, a.ctas, a);
     };
-    // Eighteen groups a thread (256 threads for the largest slice), as for the divergences (lists of 64 from 8192 rows of 16384 fp32: 148 us with 256 threads, 185
-    // with 512), four where there are few rows; and two maxima per entry of the list.
-    const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? 18 : 4) * G;
-    if (a.slice <= 32 * per && a.k <= 64) return run(std::integral_constant<int, 32>());
-    if (a.slice <= 64 * per && a.k <= 128) return run(std::integral_constant<int, 64>());
-    if (a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
+    // Many rows: eighteen groups a thread (256 threads for the largest slice), as for the divergences (lists of 64 from 8192 rows of
+    // 16384 fp32: 148 us with 256 threads, 185 with 512; from 16384 rows of 1000: 72 with one warp, 103 with four), and two
+    // maxima per entry of the list.  Few rows: what is fastest for one (of 1000, lists of 64: 5 us with 256 threads, 7.6 with 64).
+    const bool many = (int64_t)a.rows * a.ctas > device_sm_count();
+    const int per = (many ? 18 : 4) * G;
+    if (many && a.slice <= 32 * per && a.k <= 64) return run(std::integral_constant<int, 32>());
+    if (many && a.slice <= 64 * per && a.k <= 128) return run(std::integral_constant<int, 64>());
+    if (many && a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
     if (a.slice <= 256 * per && a.k <= 512) return run(std::integral_constant<int, 256>());
     return run(std::integral_constant<int, 512>());
 }
@@ -565,7 +569,10 @@ cudaError_t launch_topk_clear(const TopkArgs& a, int batch, Stream& s) {
 
 cudaError_t launch_topk(const TopkArgs& args, int rows, int dtype, Stream& s) {
     TopkArgs a = args;
-    const RowSplit sp = split_row(rows, a.V, dtype ? 2 : 4, device_sm_count());
+    // Few rows have an SM each, and one CTA to each as long as it holds them: joining lists costs more than it saves (a row of 16384 fp32,
+    // lists of 64, on 1, 2, 4, 8 CTAs: 7.3, 8.6, 8.2, 20.6 us).
+    const int sms = device_sm_count();
+    const RowSplit sp = split_row(rows, a.V, dtype ? 2 : 4, sms, rows <= sms ? ALONE_SM : SHARED_SM, false);
     a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice;
     return dtype ? run_topk<bf16>(a, s) : run_topk<float>(a, s);
 }

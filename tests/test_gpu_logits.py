@@ -607,8 +607,10 @@ def test_rows_beyond_32_bits():
     x = buf.view(rows, ld)[:, :V]
     x.copy_(_rows(1, rows, V, dtype="bf16"))
     t = _rows(2, rows, V, dtype="bf16")
-    for a, b in zip(binding.hbsjd_topk_logits(x, 20), binding.hbsjd_topk_logits(x[-30:].contiguous(), 20)):
-        assert torch.equal(a[-30:], b)
+    # (the number of rows decides how many threads sum over one: two sums, each within SUM + EXP |z| of the same value)
+    a, b = binding.hbsjd_topk_logits(x, 20), binding.hbsjd_topk_logits(x[-30:].contiguous(), 20)
+    assert torch.equal(a[0][-30:], b[0]) and torch.equal(a[1][-30:], b[1])
+    assert bool(((a[2][-30:] - b[2]).abs() <= 2 * (SUM + EXP * 60)).all())
     want = binding.hbsjd_distill(x[-30:].contiguous(), t[-30:])
     adjusted = binding.hbsjd_adjust_logits(x[-30:].contiguous(), bias=torch.ones(V, device="cuda"))
     got = binding.hbsjd_distill(x, t, grad=x)
