@@ -663,6 +663,70 @@ def test_streams_graphs_and_repeats():
         del graph
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,rows", [(40001, 700), (100000, 300), (7, 70000), (2500, 5000)])
+def test_many_rows_of_every_length(dtype, V, rows):
+    """More rows than clusters or CTAs run at once, so that each takes several, of both kinds: in work and left out."""
+    import torch
+    s, t = _rows(1, rows, V, 3.0, dtype), _rows(2, rows, V, 2.0, dtype)
+    w = torch.rand(rows, generator=_gen(3), device="cuda")
+    w[torch.rand(rows, generator=_gen(4), device="cuda") < 0.4] = 0
+    k = min(V, 50)
+    _check_topk(t, k)
+    lists = binding.hbsjd_topk_logits(t, k)
+    some = torch.randperm(rows, generator=_gen(5), device="cuda")[:60].sort().values
+    loss, grad = binding.hbsjd_distill_topk(s, *lists, w, 1.0, 0.5, 0.5)
+    ref = _distill_topk_ref(s[some], *(x[some] for x in lists), w[some], 1.0, 0.5, 0.5)
+    _compare(loss[some], grad[some], ref, dtype)
+    assert bool((loss[w == 0] == 0).all()) and not bool(grad[w == 0].any())
+    full = binding.hbsjd_distill(s, t, w, 1.0, 0.5, 0.5)
+    _compare(full[0][some], full[1][some], _distill_ref(s[some], t[some], w[some], 1.0, 0.5, 0.5), dtype)
+    assert bool((full[0][w == 0] == 0).all()) and not bool(full[1][w == 0].any())
+    # every other row against a call of its own, which deals the rows otherwise: twice the tolerance of one
+    half = slice(1, None, 2)
+    again = binding.hbsjd_distill(s[half].contiguous(), t[half].contiguous(), w[half].contiguous(), 1.0, 0.5, 0.5)
+    size = (s.double() - t.double()).abs().amax() + 20
+    assert bool(((again[0] - full[0][half]).abs() <= 4 * (SUM + EXP * 60) * size).all())
+    assert torch.equal(binding.hbsjd_adjust_logits(s, bias=torch.zeros(V, device="cuda")), s)
+
+
+def test_two_host_threads_at_once():
+    import threading
+    import torch
+    rows, V = 300, 9001
+    s, t = _rows(1, rows, V), _rows(2, rows, V)
+    side = torch.full((V,), 0.25, device="cuda"), torch.zeros(rows, 3, dtype=torch.int32, device="cuda")
+    want = _all_four(s, t, *side)
+    torch.cuda.synchronize()
+    bad = []
+
+    def work():
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got = _all_four(s, t, *side)
+                stream.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                    bad.append(1)
+        stream.synchronize()
+
+    threads = [threading.Thread(target=work) for _ in range(3)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    assert not bad
+
+
+def test_masks_of_unsigned_words():
+    import torch
+    x = _rows(1, 3, 100)
+    mask = torch.randint(-2 ** 31, 2 ** 31, (2, 4), generator=_gen(2), device="cuda").int()
+    row = torch.tensor([0, 1, 1], device="cuda").int()
+    assert torch.equal(binding.hbsjd_adjust_logits(x, mask=mask, mask_row=row),
+                       binding.hbsjd_adjust_logits(x, mask=mask.view(torch.uint32), mask_row=row))
+
+
 def test_one_row_for_all():
     import torch
     V = 2000
@@ -770,6 +834,6 @@ def test_a_step_of_distillation_from_stored_lists():
     lp = torch.log_softmax(y, -1)
     total = (0.5 * (lp.exp() * (lp - lq)).sum(-1) + 0.5 * (lq.exp() * (lq - lp)).sum(-1)).mean()
     total.backward()
-    assert abs(float(loss.mean()) - float(total)) <= 1e-4 * float(total)
+    assert abs(float(loss.mean()) - float(total.detach())) <= 1e-4 * float(total.detach())
     # fp32 products over 64 and 48 terms of logits of size 12: 1e-5 of the largest entry and more
     assert bool(((own.grad.double() - ref.grad).abs() <= 1e-4 * ref.grad.abs().max()).all())
