@@ -204,6 +204,11 @@ def _rows(what, name, x, device=None, dtype=None, shape=None, written=False):
     return x.data_ptr(), ld, _types.get(own)
 
 
+def _plain(x, device, dtype):
+    """Whether x is a contiguous matrix of this type on this device: what needs no look at its strides."""
+    return isinstance(x, _torch.Tensor) and x.dtype == dtype and x.device == device and x.is_contiguous() and x.dim() == 2
+
+
 def _vector(what, name, x, device, dtype, n):
     """Pointer of a contiguous vector, or None."""
     if x is None:
@@ -261,7 +266,12 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
         u, ld_u, _ = _rows(what, "logits_u", logits_u, device, logits.dtype, shape)
     words, ld_mask, masks = None, 0, 0
     if mask is not None:
-        words, ld_mask, _ = _rows(what, "mask", mask, device, i32 if getattr(mask, "dtype", None) == i32 else _torch.uint32)
+        if _plain(mask, device, i32):
+            words = mask.data_ptr()
+            ld_mask = mask.shape[1]
+        else:
+            words, ld_mask, _ = _rows(what, "mask", mask, device,
+                                      i32 if getattr(mask, "dtype", None) == i32 else _torch.uint32)
         masks = mask.shape[0]
         if mask.shape[1] < (V + 31) // 32:
             _refuse(what, f"mask has {mask.shape[1]} words for {V} entries")
@@ -271,7 +281,11 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
             _refuse(what, "mask: rows overlap")
     tok, ld_history, sequences, cap = None, 0, 0, 0
     if history is not None:
-        tok, ld_history, _ = _rows(what, "history", history, device, i32, written=True)
+        if _plain(history, device, i32):
+            tok = history.data_ptr()
+            ld_history = history.shape[1]
+        else:
+            tok, ld_history, _ = _rows(what, "history", history, device, i32, written=True)
         sequences, cap = history.shape
         if not sequences or not cap:
             tok = None
@@ -324,7 +338,7 @@ def _distill(what, entry, logits_s, s, ld_s, dtype_s, teacher, dtype_t, ld_t, k,
     else:
         g, ld_g = None, 0
     w = _vector(what, "weight", weight, device, _torch.float32, rows)
-    loss = logits_s.new_empty((rows,), dtype=_torch.float32)
+    loss = logits_s.new_empty((rows,), dtype=_torch.float32) if w is None else _torch.empty_like(weight)
     if rows:
         d = hbsjd_distill_desc(rows, V, dtype_s, dtype_t, k, 0, ld_s, ld_t, ld_g, temperature, forward, reverse, 0)
         _call(what, entry, device, d, s, *teacher, w, loss.data_ptr(), g)
@@ -357,14 +371,13 @@ def hbsjd_distill_topk(logits_s, values, indices, rest=None, weight=None, temper
     if stream is not None or device.index != _torch.cuda.current_device():
         return _elsewhere(hbsjd_distill_topk, what, logits_s, stream,
                           (logits_s, values, indices, rest, weight, temperature, forward, reverse, want_grad, grad), {})
-    v, ld_v, _ = _rows(what, "values", values, device, _torch.float32)
-    rows, k = values.shape
-    i, ld_i, _ = _rows(what, "indices", indices, device, _torch.int32, values.shape)
-    if rows != logits_s.shape[0] or ld_v != k or ld_i != k:
-        _refuse(what, f"values and indices have to be contiguous, with {logits_s.shape[0]} rows")
+    rows = logits_s.shape[0]
+    if not (_plain(values, device, _torch.float32) and _plain(indices, device, _torch.int32) and
+            values.shape == indices.shape and values.shape[0] == rows):
+        _refuse(what, f"values and indices have to be contiguous matrices of fp32 and int32 with {rows} rows on {device}")
     r = _vector(what, "rest", rest, device, _torch.float32, rows)
-    return _distill(what, load().hbsjd_distill_topk, logits_s, s, ld_s, dtype_s, (v, i, r), 0, 0, k, weight, temperature,
-                    forward, reverse, want_grad, grad)
+    return _distill(what, load().hbsjd_distill_topk, logits_s, s, ld_s, dtype_s, (values.data_ptr(), indices.data_ptr(), r),
+                    0, 0, values.shape[1], weight, temperature, forward, reverse, want_grad, grad)
 
 
 class Context:
