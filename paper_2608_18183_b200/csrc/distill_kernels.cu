@@ -222,6 +222,16 @@ __device__ __forceinline__ float log_add(float x, float y) {
     return m == -INFINITY ? x + y : fmaf(LN2, lg2(ex2((x - m) * LOG2E) + ex2((y - m) * LOG2E)), m);
 }
 
+// log(1 + e^r), to its own last digits where it is small too: log(1 + z) = 2 (u + u^3 / 3 + u^5 / 5 ...) with u = z / (2 + z), where
+// z <= 1 leaves 1e-8 of it behind u^15.
+__device__ __forceinline__ float softplus(float r) {
+    const float z = ex2(-fabsf(r) * LOG2E), u = __fdividef(z, 2.f + z), u2 = u * u;
+    float f = 1.f / 15;
+#pragma unroll
+    for (int i = 13; i > 0; i -= 2) f = fmaf(f, u2, 1.f / i);
+    return fmaf(2.f * u, f, fmaxf(r, 0.f));
+}
+
 // What one warp makes of a row's sums for all: the others would only take its issue slots (each warp for itself: 485 us in
 // place of 400 for 16384 rows of 16384).
 struct ListCoefs {
@@ -400,7 +410,9 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                 const float Lx = log_add(xl, xo), Ly = log_add(yl, yo);
                 const float ql = ex2((xl - Lx) * LOG2E), qo = ex2((xo - Lx) * LOG2E);
                 const float pl = ex2((yl - Ly) * LOG2E), po = ex2((yo - Ly) * LOG2E);
-                const float ratio = (xo - Lx) - (yo - Ly);                // log of qo / po
+                // log of qo / po: by what the list leaves of each, since near 1 the logarithms of both are differences of larger ones
+                // (one listed token of mass 1e-3: the loss was 1.7e-4 off)
+                const float ratio = softplus(yl - yo) - softplus(xl - xo);
                 const float shift = v.ms == -INFINITY ? 0.f : Mx - v.ms;  // (the sums of d are against v.ms)
                 // a mass of zero adds nothing, whatever its logarithm is (NaN passes)
                 float kl_pq = 0.f, kl_qp = 0.f;
@@ -410,7 +422,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                 if (qo != 0.f) kl_qp += qo * ratio;
                 if (lane == 0) {
                     // others: q_v (a (1 - po / qo) + b (ratio - KL(q || p))), with q_v / qo their share of u.z
-                    float k0 = a.forward * (qo - po);
+                    float k0 = a.forward * (ql + pl < qo + po ? pl - ql : qo - po);
                     if (a.reverse != 0.f && qo != 0.f) k0 += a.reverse * qo * (ratio - kl_qp);
                     k0 = u.z == 0.f ? 0.f : __fdividef(k0 * (w * inv_tau), u.z);
                     coefs = {Mx, My, Lx, Ly, kl_qp, u.m == -INFINITY ? 0.f : u.m, k0, empty};

@@ -413,6 +413,43 @@ def test_distill_topk_shapes(dtype, V, k, rows, pad, shift):
     _compare(loss, grad, _distill_topk_ref(s, values, indices, rest, w, 1.0, 1.0, 0.0), dtype)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("heavy", [False, True])
+def test_divergences_that_are_small_keep_their_digits(dtype, heavy):
+    """A listed token of little mass, or of all but a little.  The loss moves with the logarithms rx, ry of the listed mass over the others'
+    by q_l q_o (rx - ry) drx + (p_l - q_l) dry for KL(q || p), and with the names changed for KL(p || q), however large they are;
+    rx is off by what its mass is (SUM) and by the roundings of its logits, its logarithm and the rest (10 halves of its
+    parts, none larger than the row's largest logits' size in temperatures, the teacher's rest and log V = 11)."""
+    import torch
+    V, rows, tau = 50021, 24, 2.0
+    s = _rows(V, rows, V, 1.0, dtype)
+    at = (torch.arange(rows, device="cuda") * 1999 + 7)
+    s[torch.arange(rows, device="cuda"), at] = (torch.linspace(-6, 4, rows, device="cuda") + (38 if heavy else 0)).to(s.dtype)
+    values = s.float().gather(1, at[:, None]) + torch.where(torch.arange(rows, device="cuda") % 2 == 0, 1.5, -1.5)[:, None]
+    x = s.double() / tau
+    xl = x.gather(1, at[:, None])[:, 0]
+    xo = torch.logsumexp(x.scatter(1, at[:, None], NEG), -1)
+    rest = (xo + 0.25).float()
+    yl, yo = values[:, 0].double() / tau, rest.double()
+    rx, ry = xl - xo, yl - yo
+    lql, lqo, lpl, lpo = (torch.nn.functional.logsigmoid(v) for v in (rx, -rx, ry, -ry))
+    ql, qo, pl, po = lql.exp(), lqo.exp(), lpl.exp(), lpo.exp()
+    # sum f log(f / g) as a sum of terms that are none below 0: 64 bits keep all that is asked for
+    kl = lambda f, lf, g, lg: sum(a * (b - d) - a + c for a, b, c, d in zip(f, lf, g, lg))
+    F, R = kl((pl, po), (lpl, lpo), (ql, qo), (lql, lqo)), kl((ql, qo), (lql, lqo), (pl, po), (lpl, lpo))
+    size = torch.stack([xl.abs(), xo.abs(), yl.abs(), yo.abs()]).amax(0) + 11
+    dr = SUM + 10 * HALF["fp32"] * size
+    dif, mass = (rx - ry).abs(), (pl - ql).abs()
+    tF, tR = dr * (pl * po * dif + mass), dr * (ql * qo * dif + mass)
+    # the listed token's term is its mass times a sum of logarithms, the others' theirs times one that is about the listed mass
+    term = lambda f: 8 * HALF["fp32"] * f * (dif + size)
+    for a, b, want, tol in ((1.0, 0.0, F, tF + term(pl)), (0.0, 1.0, R, tR + term(ql))):
+        loss, _ = binding.hbsjd_distill_topk(s, values, at[:, None].int(), rest, None, tau, a, b)
+        assert bool(((loss.double() - want).abs() <= tol).all()), ((loss.double() - want) / tol, want)
+        if not heavy:
+            assert float((tol / want).max()) < 1e-3              # (differences of logarithms near 11 would be off by 1e-6, of 1e-7 to 1e-4)
+
+
 def test_distill_topk_lists_with_gaps_and_repeats():
     """Entries that count for nothing (-inf, tokens outside the vocabulary, tokens listed before), lists without an entry, in
     rows held by one CTA and by several."""
