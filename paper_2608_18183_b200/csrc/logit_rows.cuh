@@ -78,8 +78,9 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// (not .aligned: rows end in branches by lane, and a warp may reach these in parts)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // address in CTA `rank`'s shared memory of what lies at `p` in this CTA's
 __device__ __forceinline__ uint32_t remote_smem(const void* p, uint32_t rank) {
     uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
