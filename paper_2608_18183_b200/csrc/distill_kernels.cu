@@ -354,6 +354,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                 v.ms = fmaxf(v.ms, x);
                 v.mt = fmaxf(v.mt, val[i]);
             });
+            __syncwarp();  // (other lanes sum over their places)
             if (__any_sync(0xffffffffu, any)) {
                 v.share();
                 const float os = v.ms == -INFINITY ? 0.f : v.ms, ot = v.mt == -INFINITY ? 0.f : v.mt;

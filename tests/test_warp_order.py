@@ -30,3 +30,14 @@ def test_cluster_barriers_that_whole_warps_have_to_reach():
         assert calls, f
         for at in calls:
             assert re.search(r"__syncthreads\(\);\s*(if \(PAIR\) )?$", rest[:at]), (f, rest[at - 80:at])
+
+
+def test_listed_tokens_leave_the_row_before_other_lanes_sum_over_it():
+    """A lane takes a listed token out of the staged row; other lanes read its place.  Votes, maxima and shuffles order no shared
+    memory between them: a barrier of the warp has to stand in between."""
+    text = _source("distill_kernels.cu")
+    body = text[text.index(" k_distill_topk("):]
+    out = [m.end() for m in re.finditer(r"ss\[e\] = from_f<TS>\(-INFINITY\);", body)]
+    assert len(out) == 1
+    behind = body[out[0]:]
+    assert "__syncwarp();" in behind[:re.search(r"get<G>\(ss\b", behind).start()]
