@@ -145,15 +145,19 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
                             k2 = f * a.forward;
                 if (empty) {
                     put_zeros(g, lo, hi);
-                } else if (special[turn]) {
+                } else if (special[turn] || !(fabsf(v.ms) < 1e30f && fabsf(v.mt) < 1e30f)) {
                     for (int e = lo + lane; e < hi; e += 32) {
                         const float xo = to_f<TS>(ss[p.P + e]) - v.ms, yo = to_f<TT>(st[p.P + e]) - v.mt;
                         const float q = ex2(fmaf(xo, c, -ls)), r = ex2(fmaf(yo, c, -lt)), m = rev ? fmaf(k1, xo - yo, k0) : k0;
                         g[e] = from_f<TS>(fmaf(-k2, r, q == 0.f ? 0.f : q * m));
                     }
                 } else {
-                    const f32x2 os = both(-v.ms), ot = both(-v.mt), c2 = both(c), minus = both(-1.f), nls = both(-ls), nlt = both(-lt);
-                    const f32x2 K0 = both(k0), K1 = both(k1), K2 = both(-k2);
+                    // At an entry of the type's lowest value d is about that, and finite, since both references are far less; but k1 above 1
+                    // would take the product to infinity, beside a q of zero.  q takes the power of two that k1 has too much.
+                    const int up = min(max((int)(__float_as_uint(fabsf(k1)) >> 23) - 126, 0), 126);
+                    const float down = __uint_as_float((uint32_t)(127 - up) << 23);
+                    const f32x2 os = both(-v.ms), ot = both(-v.mt), c2 = both(c), minus = both(-1.f), nls = both((float)up - ls), nlt = both(-lt);
+                    const f32x2 K0 = both(k0 * down), K1 = both(k1 * down), K2 = both(-k2);
                     const auto gradient = [&](float(&x)[G], const float(&y)[G]) {
 #pragma unroll
                         for (int i = 0; i < G; i += 2) {

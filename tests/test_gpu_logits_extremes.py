@@ -1,0 +1,68 @@
+"""Divergences of rows that are masked by finite values, or come at temperatures far from one: against 64 bits."""
+import pytest
+
+from paper_2608_18183_b200 import binding
+from tests.test_gpu_logits import EXP, HALF, SUM, _compare, _distill_ref, _gen, _rows, _t
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,rows", [(1000, 7), (16384, 6), (16384, 320), (40001, 160)])
+def test_gradients_where_the_lowest_value_masks_the_student(dtype, V, rows):
+    """weight * reverse / temperature^2 above 1 times the lowest value is beyond the type, and such an entry has no share: its
+    gradient is -weight forward p / temperature, which is no NaN.  The lowest value on the student alone, against -1e9, against
+    itself, and over a block that holds whole parts of the row."""
+    import torch
+    low = torch.finfo(_t(dtype)).min
+    s, t = _rows(1, rows, V, 3.0, dtype), _rows(2, rows, V, 2.0, dtype)
+    hide = torch.rand(rows, V, generator=_gen(3), device="cuda") < 0.3
+    hide[:, 0] = False
+    block = torch.zeros(rows, V, dtype=torch.bool, device="cuda")
+    block[:, V // 4:V - V // 4] = True
+    kind = (torch.arange(rows, device="cuda") % 6)[:, None]
+    here = torch.where(kind < 3, hide, block)
+    t = torch.where(here & (kind % 3 == 1), -1e9, t.float()).to(t.dtype)
+    t = torch.where(here & (kind % 3 == 2), low, t.float()).to(t.dtype)
+    s = torch.where(here, low, s.float()).to(s.dtype)
+    for weight, tau, a, b in ((1.0, 0.7, 0.0, 1.0), (1.0, 0.5, 0.5, 0.5), (2.0, 1.0, 0.0, 1.0), (1.0, 0.7, 0.5, 0.5), (1.0, 1.0, 0.0, 1.0),
+                              (0.5, 1.0, 0.5, 0.5), (-3.0, 1.0, 0.2, 0.8), (1.0, 0.7, 1.0, 0.0), (50.0, 0.1, 0.1, 0.9)):
+        w = torch.full((rows,), weight, device="cuda")
+        loss, grad = binding.hbsjd_distill(s, t, w, tau, a, b)
+        want, g, tl, tg = _distill_ref(s, t, w, tau, a, b)
+        # The reference drops shares below 2^-126; the kernel may count those from 2^-126 / k1 on, with k1 = 2 weight reverse / tau^2 and
+        # more: an entry of such a share q is off by q (a + b (|r| + KL(q || p))) weight / tau, rounded (2^-8 of it in bf16), and by
+        # the sums' error of that (below 2^-8, too); no other is.  A teacher's share near 2^-126 may fall either way: a p weight / tau.
+        lq, lp = torch.log_softmax(s.double() / tau, -1), torch.log_softmax(t.double() / tau, -1)
+        q, r = lq.exp(), (lq - lp).abs()
+        edge = (q < 1.01 * 2.0 ** -126) & (q * (2 * abs(weight) * b / tau ** 2 + 2) > 2.0 ** -126)
+        more = torch.where(edge, 1.01 * q * (a + b * (r + (q * r).sum(-1, keepdim=True))) * abs(weight) / tau, 0.0)
+        more = more + 1.01 * 2.0 ** -126 * a * abs(weight) / tau
+        tg = tg + more
+        assert bool(torch.isfinite(grad).all()), (weight, tau, a, b, torch.isnan(grad).sum(-1).unique())
+        both = torch.arange(rows, device="cuda") % 3 != 0       # (the loss too, where forward KL does not pass what fp32 holds)
+        if a == 0:
+            both[:] = True
+        _compare(loss[both], grad[both], tuple(x[both] for x in (want, g, tl, tg)), dtype)
+        # on the student alone: a KL(p || q) beyond fp32's reach; the gradients stay
+        if a:
+            assert bool((loss[~both] > 1e30).all())
+            err = (grad.double() - g).abs()
+            # (the tolerance without forward KL's huge logarithms)
+            p = lp.exp()
+            fin = torch.where(q > 0, (s.double() - t.double()).abs() / tau, 0.0)
+            size = a * (q + p) + b * q * (fin + (q * fin).sum(-1, keepdim=True) + 1)
+            tol = abs(weight) / tau * size * (2 * SUM + EXP * 150) + HALF[dtype] * g.abs() + more + 1e-37
+            assert bool((err <= tol)[~both].all()), float((err / tol)[~both].max())
+
+
+def test_the_lowest_value_beside_logits_that_are_nearly_as_large():
+    """The lowest value less a reference of 2e31 is infinite, and the entry has no share all the same."""
+    import torch
+    for V, rows in ((16384, 4), (16384, 320)):
+        s, t = _rows(1, rows, V), _rows(2, rows, V, 2.0)
+        s[:, 100], t[:, 100] = 2e31, 2e31
+        s[:, 9000:9004] = torch.finfo(torch.float32).min
+        w = torch.full((rows,), 2.0, device="cuda")
+        loss, grad = binding.hbsjd_distill(s, t, w, 0.7, 0.5, 0.5)
+        assert not bool(loss.any()) and not bool(grad.any())    # both have all mass on one token
