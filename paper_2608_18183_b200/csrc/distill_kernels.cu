@@ -145,11 +145,13 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
                             k2 = f * a.forward;
                 if (empty) {
                     put_zeros(g, lo, hi);
-                } else if (special[turn] || !(fabsf(v.ms) < 1e30f && fabsf(v.mt) < 1e30f)) {
+                } else if (special[turn] || !(fabsf(v.ms) < 1e30f && fabsf(v.mt) < 1e30f && fabsf(k0) + fabsf(k1) + fabsf(k2) < 1e30f)) {
+                    // (the factors one by one: temperatures below 1e-15 leave none of their products)
                     for (int e = lo + lane; e < hi; e += 32) {
                         const float xo = to_f<TS>(ss[p.P + e]) - v.ms, yo = to_f<TT>(st[p.P + e]) - v.mt;
-                        const float q = ex2(fmaf(xo, c, -ls)), r = ex2(fmaf(yo, c, -lt)), m = rev ? fmaf(k1, xo - yo, k0) : k0;
-                        g[e] = from_f<TS>(fmaf(-k2, r, q == 0.f ? 0.f : q * m));
+                        const float q = ex2(fmaf(xo, c, -ls)), r = ex2(fmaf(yo, c, -lt));
+                        const float m = rev ? fmaf(a.reverse, (xo - yo - __fdividef(v.as, v.zs)) * inv_tau, a.forward) : a.forward;
+                        g[e] = from_f<TS>(fmaf(-a.forward, r, q == 0.f ? 0.f : q * m) * inv_tau * w);
                     }
                 } else {
                     // At an entry of the type's lowest value d is about that, and finite, since both references are far less; but k1 above 1

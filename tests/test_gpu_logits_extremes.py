@@ -62,7 +62,29 @@ def test_the_lowest_value_beside_logits_that_are_nearly_as_large():
     for V, rows in ((16384, 4), (16384, 320)):
         s, t = _rows(1, rows, V), _rows(2, rows, V, 2.0)
         s[:, 100], t[:, 100] = 2e31, 2e31
-        s[:, 9000:9004] = torch.finfo(torch.float32).min
+        s[:, 9000:9004], t[:, 9000:9004] = torch.finfo(torch.float32).min, -1e9
         w = torch.full((rows,), 2.0, device="cuda")
         loss, grad = binding.hbsjd_distill(s, t, w, 0.7, 0.5, 0.5)
         assert not bool(loss.any()) and not bool(grad.any())    # both have all mass on one token
+
+
+@pytest.mark.parametrize("V,rows", [(9, 4), (1001, 320), (16385, 5)])
+def test_temperatures_near_none(V, rows):
+    """At a temperature far below the logits' differences both distributions are one token each, and the gradient is
+    weight forward / temperature at the student's less the same at the teacher's: that of KL(q || p) is q (d - E_q d), which is none."""
+    import torch
+    s, t = _rows(1, rows, V), _rows(2, rows, V, 2.0)
+    t[::2, 3], s[::2, 3] = 50.0, 50.0                           # (every other row: the same token)
+    w = torch.full((rows,), 0.5, device="cuda")
+    at = torch.arange(rows, device="cuda")
+    for tau in (1e-10, 1e-20, 1e-30):
+        for a, b in ((1.0, 0.0), (0.0, 1.0), (0.5, 0.5)):
+            _, grad = binding.hbsjd_distill(s, t, w, tau, a, b)
+            want = torch.zeros(rows, V, dtype=torch.float64, device="cuda")
+            want[at, s.argmax(-1)] += 0.5 * a / tau
+            want[at, t.argmax(-1)] -= 0.5 * a / tau
+            # shares of 1 by ex2 and lg2, temperature and its inverse rounded, products; and d - E_q d of two that are alike, each
+            # rounded by its size
+            tol = (2 * SUM + 8 * HALF["fp32"]) * want.abs()
+            tol[at, s.argmax(-1)] += 0.5 * b / tau * 4 * HALF["fp32"] * ((s - t).abs().amax(-1) * 2 / tau).double()
+            assert bool(torch.isfinite(grad).all()) and bool(((grad.double() - want).abs() <= tol).all()), (tau, a, b)
