@@ -2,7 +2,7 @@
 import pytest
 
 from paper_2608_18183_b200 import binding
-from tests.test_gpu_logits import EXP, HALF, SUM, _compare, _distill_ref, _gen, _rows, _t
+from tests.test_gpu_logits import EXP, HALF, NEG, SUM, _compare, _distill_ref, _gen, _rows, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +88,56 @@ def test_temperatures_near_none(V, rows):
             tol = (2 * SUM + 8 * HALF["fp32"]) * want.abs()
             tol[at, s.argmax(-1)] += 0.5 * b / tau * 4 * HALF["fp32"] * ((s - t).abs().amax(-1) * 2 / tau).double()
             assert bool(torch.isfinite(grad).all()) and bool(((grad.double() - want).abs() <= tol).all()), (tau, a, b)
+
+
+def _list_ref(s, values, indices, rest, tau, a, b):
+    """Loss, gradient and bounds of their errors over the listed tokens and the others, whose shares are taken against their own
+    largest: at -1e30 64 bits keep nothing of a logarithm that is added to a logit."""
+    import torch
+    x = s.double()
+    z = (x - x.amax(-1, keepdim=True)) / tau
+    at = indices.long()
+    zo = z.scatter(1, at, NEG)
+    mo = zo.amax(-1, keepdim=True)
+    share = torch.exp(zo - mo)
+    no = share.sum(-1, keepdim=True)
+    lq = torch.log_softmax(torch.cat([z.gather(1, at), mo + no.log()], 1), -1)
+    lp = torch.log_softmax(torch.cat([values.double() / tau, rest.double()[:, None]], 1), -1)
+    q, p, r = lq.exp(), lp.exp(), lq - lp
+    F, R = (-p * r).sum(-1, keepdim=True), (q * r).sum(-1, keepdim=True) if b else 0.0
+    g = a * (q - p) + (b * q * (r - R) if b else 0.0)
+    # masses of sums and exponentials: each outcome's share is off by SUM and by EXP times its logarithm, which is below 90 or not there
+    size = a * (q + p) + (b * q * (r.abs() + R.abs() + 1) if b else 0.0)
+    full = lambda y: (y[:, -1:] * share / no).scatter(1, at, y[:, :-1])
+    loss = (a * F + b * R)[:, 0]
+    tl = ((a * p + b * q) * (r.abs() + 1)).sum(-1)
+    return loss, full(g) / tau, (2 * SUM + 90 * EXP) * tl, (3 * SUM + 90 * EXP) * full(size) / tau
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,rows,shift", [(9, 3, 0), (1001, 300, 1), (16385, 4, 0), (16385, 300, 3)])
+def test_lists_beside_others_of_one_very_low_value(dtype, V, rows, shift):
+    """-1e30, which many programs mask with, on all tokens or on all that are not listed: each has the same share, whatever fills
+    the row up to whole groups.  And temperatures at which such a value is not low."""
+    import torch
+    k = 3
+    indices = torch.stack([torch.randperm(V, generator=_gen(r), device="cuda")[:k] for r in range(rows)]).int()
+    values = torch.randn(rows, k, generator=_gen(1), device="cuda")
+    rest = torch.randn(rows, generator=_gen(2), device="cuda")
+    low = _rows(0, rows, V, 0.0, dtype, 0, shift).fill_(-1e30)
+    cases = [(low, 1.0), (low, 100.0)]
+    some = _rows(0, rows, V, 0.0, dtype, 0, shift).fill_(-1e30)
+    some.scatter_(1, indices.long(), torch.randn(rows, k, generator=_gen(3), device="cuda").to(some.dtype))
+    cases.append((some, 1.0))
+    cases += [(_rows(4, rows, V, 3.0, dtype, 0, shift), tau) for tau in (1e28, 1e29, 1e30, 3e31, 1e36)]
+    for s, tau in cases:
+        y = values * tau if tau > 1e3 else values
+        for a, b in ((1.0, 0.0), (0.5, 0.5)):
+            loss, grad = binding.hbsjd_distill_topk(s, y, indices, rest, None, tau, a, b)
+            want, g, tl, tg = _list_ref(s, y, indices, rest, tau, a, b)
+            gone = want > 1e25                                  # (the student has nothing where the teacher's rest has)
+            assert torch.equal(gone, loss > 1e25)
+            assert bool(((loss.double() - want).abs() <= tl + HALF["fp32"] * want)[~gone].all()), (tau, a, b)
+            if b and bool(gone.any()):
+                continue                                        # (KL(q || p) takes no part in what is asked here)
+            assert bool(((grad.double() - g).abs() <= tg + HALF[dtype] * g.abs() + 1e-37).all()), (tau, a, b)
