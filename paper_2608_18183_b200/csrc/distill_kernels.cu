@@ -105,8 +105,11 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
                 }
                 v.zs = sum2(zs), v.zt = sum2(zt), v.as = sum2(as), v.at = sum2(at);
             }
-            // (false for NaN, infinities, and sums that a factor could not bring down again)
-            const bool fine = v.zs < 1e12f && v.zt < 1e12f && fabsf(v.as) < 1e30f && fabsf(v.at) < 1e30f;
+            // (false for NaN, infinities, and sums that a factor could not bring down again; and where the fill beside the row's ends
+            // would have a share: a row of values as low as it, a temperature so high)
+            const bool apart = (p.inner() == p.j0 && p.outer() == p.j1) || ((v.ms - to_f<TS>(from_f<TS>(PAD))) * c > 150.f &&
+                                                                            (v.mt - to_f<TT>(from_f<TT>(PAD))) * c > 150.f);
+            const bool fine = v.zs < 1e12f && v.zt < 1e12f && fabsf(v.as) < 1e30f && fabsf(v.at) < 1e30f && apart;
             if (!__all_sync(0xffffffffu, fine) || !__any_sync(0xffffffffu, v.zs > 0.f) || !__any_sync(0xffffffffu, v.zt > 0.f)) {
                 if (lane == 0 && p.j0 < p.j1) special[turn] = 1;
                 v = Pair::none();

@@ -141,3 +141,24 @@ def test_lists_beside_others_of_one_very_low_value(dtype, V, rows, shift):
             if b and bool(gone.any()):
                 continue                                        # (KL(q || p) takes no part in what is asked here)
             assert bool(((grad.double() - g).abs() <= tg + HALF[dtype] * g.abs() + 1e-37).all()), (tau, a, b)
+
+
+@pytest.mark.parametrize("ds,dt", [("fp32", "fp32"), ("bf16", "bf16"), ("fp32", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("V,rows,shift", [(9, 3, 0), (1001, 300, 1), (16385, 4, 0), (16385, 300, 3)])
+def test_rows_of_one_very_low_value_and_temperatures_beyond_it(ds, dt, V, rows, shift):
+    """As above, of two whole rows: uniform at -1e30 on one side or both; at temperatures from 1e28 on both rows are uniform, and the
+    divergence is none, whatever the two types make of the value that fills them up."""
+    import torch
+    s, t = _rows(1, rows, V, 3.0, ds, 0, shift), _rows(2, rows, V, 2.0, dt, 0, shift)
+    low_s, low_t = _rows(0, rows, V, 0.0, ds, 0, shift).fill_(-1e30), _rows(0, rows, V, 0.0, dt, 0, shift).fill_(-1e30)
+    w = torch.ones(rows, device="cuda")
+    for a, b in ((1.0, 0.0), (0.0, 1.0), (0.5, 0.5)):
+        for x, y in ((low_s, t), (s, low_t), (low_s, low_t)):
+            for tau in (1.0, 0.7):
+                # (-1e30 / tau is uniform too, and 64 bits take its maximum off first)
+                _compare(*binding.hbsjd_distill(x, y, w, tau, a, b), _distill_ref(x, y, w, tau, a, b), ds)
+        for tau in (1e28, 1e29, 1e30, 3e31, 1e36):
+            loss, grad = binding.hbsjd_distill(s, t, None, tau, a, b)
+            # |d| / tau is below 40 / 1e28: the loss has its sums' error of that, and the gradient q - p of two equal masses
+            assert float(loss.abs().max()) <= 40 / tau, (tau, a, b, float(loss.abs().max()))
+            assert float(grad.abs().max()) * tau <= (3 * SUM + 20 * EXP) / V, (tau, a, b)
