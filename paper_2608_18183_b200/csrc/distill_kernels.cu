@@ -26,6 +26,49 @@ __device__ __forceinline__ int common_phase(const TS* s, const TT* t) {
     return sizeof(TS) == 4 && sizeof(TT) == 2 && Pt % 4 == P ? Pt : P;
 }
 
+// Divergences below this are summed as terms none of which is negative.  As delta - E_p d the loss is off by what two sums' quotient and
+// its logarithm are, up to 7e-7 whatever the divergence is: 5e-5 of it here, more than all of a KL of 5e-7 (7e-5 of that as these terms).
+constexpr float NEAR = 1.f / 64;
+
+// f of e^r - 1 - r (x = +r) and e^-r - 1 + r (x = -r) over r^2 for |r| < 3/4: series whose next terms are below 7e-7 of them.
+struct Bregman {
+    float r2, even, odd;
+    __device__ __forceinline__ explicit Bregman(float r) : r2(r * r) {
+        even = fmaf(r2, fmaf(r2, fmaf(r2, 1.f / 40320, 1.f / 720), 1.f / 24), 0.5f);
+        odd = r * fmaf(r2, fmaf(r2, 1.f / 5040, 1.f / 120), 1.f / 6);
+    }
+    __device__ __forceinline__ float up() const { return r2 * (even + odd); }
+    __device__ __forceinline__ float down() const { return r2 * (even - odd); }
+    __device__ __forceinline__ static bool reaches(float r) { return fabsf(r) < 0.75f; }
+};
+
+// A warp's sums of p (e^r - 1 - r) (as zs) and q (e^-r - 1 + r) (as zt) with r = log q / p, which are KL(p || q) and KL(q || p) since p and q
+// sum to one.  An error that all r share counts by the square: none of the masses' logarithms has to be good.
+template <typename TS, typename TT, int G, int WARPS>
+__device__ __forceinline__ Pair near_sums(const TS* ss, const TT* st, const Part<G, WARPS>& p, const Pair& v, float c, float inv_tau, float ls,
+                                          float lt, float delta) {
+    Pair h = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int j = p.j0 + (threadIdx.x & 31); j < p.j1; j += 32) {
+        float x[G], y[G];
+        get<G>(ss + j * G, x);
+        get<G>(st + j * G, y);
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const float xo = x[i] - v.ms, yo = y[i] - v.mt, r = fmaf(xo - yo, inv_tau, -delta);
+            const float eq = ex2(fmaf(xo, c, -ls)), ep = ex2(fmaf(yo, c, -lt));
+            const Bregman b(r);
+            // (far from one another as they are; no mass on either side: r is not looked at)
+            const float f = Bregman::reaches(r) ? ep * b.up() : eq - (ep == 0.f ? 0.f : ep * (1.f + r));
+            const float g = Bregman::reaches(r) ? eq * b.down() : ep - (eq == 0.f ? 0.f : eq * (1.f - r));
+            const bool in = j * G + i >= p.P && j * G + i < p.P + p.n;  // (a row as low as what fills it up gives that a share)
+            h.zs += in ? f : 0.f;
+            h.zt += in ? g : 0.f;
+        }
+    }
+    return h;
+}
+
 template <typename TS, typename TT, int THREADS, int PER_SM>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
     constexpr int G = sizeof(TS) == 2 && sizeof(TT) == 2 ? 8 : 4, WARPS = THREADS / 32;
@@ -132,14 +175,27 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
             const bool empty = v.zs == 0.f || v.zt == 0.f, rev = a.reverse != 0.f;
             // (against the maxima: their difference is in neither d nor delta)
             const float A_q = __fdividef(v.as, v.zs) * inv_tau, ls = lg2(v.zs), lt = lg2(v.zt);
-            if (a.loss && blockIdx.x % a.ctas == 0 && threadIdx.x == 0) {
+            if (a.loss) {
                 float loss = 0.f;
                 if (!empty) {
-                    if (a.forward != 0.f) loss -= a.forward * (__fdividef(v.at, v.zt) * inv_tau);
+                    const float A_p = __fdividef(v.at, v.zt) * inv_tau;
+                    const float delta = v.zs == v.zt ? 0.f : LN2 * lg2(__fdividef(v.zs, v.zt));  // (equal rows: none)
+                    if (a.forward != 0.f) loss -= a.forward * A_p;
                     if (rev) loss += a.reverse * A_q;
-                    if (a.forward != a.reverse) loss += (a.forward - a.reverse) * (LN2 * (ls - lt));
+                    if (a.forward != a.reverse) {
+                        loss += (a.forward - a.reverse) * delta;
+                        // (the same for all CTAs of the row, whose sums are the same bits; at equal weights delta takes no part)
+                        if ((a.forward == 0.f || delta - A_p < NEAR) && (!rev || A_q - delta < NEAR)) {
+                            const Pair h = near_sums<TS, TT, G, WARPS>(ss, st, p, v, c, inv_tau, ls, lt, delta);
+                            parity ^= 1;
+                            post<WARPS>(h, slots + parity * places, a.ctas, rank);
+                            posted(a.ctas);
+                            const Pair sum = collect(slots + parity * places, places, c);
+                            loss = (a.forward == 0.f ? 0.f : a.forward * sum.zs) + (rev ? a.reverse * sum.zt : 0.f);
+                        }
+                    }
                 }
-                a.loss[row] = loss;
+                if (rank == 0 && threadIdx.x == 0) a.loss[row] = loss;
             }
             if (g) {
                 const int Pg = phase_of(g) % G;  // the gradient is written wide, whatever the others' alignment
