@@ -86,10 +86,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
     Pair* slots = (Pair*)(st + a.slice + 16);  // [2][places], by turns: a CTA may be a row ahead of others
     if (threadIdx.x < 3) special[threadIdx.x] = 0;
     __syncthreads();
-    if (a.ctas > 1) {
-        cluster_arrive();
-        cluster_wait();  // every CTA of the rows runs
-    }
+    if (a.ctas > 1) cluster_barrier();  // every CTA of the rows runs
     const auto weight = [&](int row) { return row >= a.rows ? 0.f : a.weight ? __ldg(a.weight + row) : 1.f; };
     const auto fetch = [&](int row) {
         const TS* s = (const TS*)a.s + (int64_t)row * a.ld_s + v0;
@@ -329,10 +326,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     for (int i = threadIdx.x; i < words; i += THREADS) seen[i] = 0;
     if (threadIdx.x < 2) repeated[threadIdx.x] = 0;
     __syncthreads();
-    if (a.ctas > 1) {
-        cluster_arrive();
-        cluster_wait();  // every CTA of the rows runs
-    }
+    if (a.ctas > 1) cluster_barrier();  // every CTA of the rows runs
     const auto weight = [&](int row) { return row >= a.rows ? 0.f : a.weight ? __ldg(a.weight + row) : 1.f; };
     const auto fetch = [&](int row) {
         const TS* s = (const TS*)a.s + (int64_t)row * a.ld_s + v0;

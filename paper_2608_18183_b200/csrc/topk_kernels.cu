@@ -116,10 +116,7 @@ __global__ void __launch_bounds__(THREADS, topk_ctas<THREADS>()) k_topk(TopkArgs
         found = bad = big = 0;
         least_key = 0xffffffffu, top_key = 0;
     }
-    if (a.ctas > 1) {
-        cluster_arrive();
-        cluster_wait();  // every CTA of the rows runs
-    }
+    if (a.ctas > 1) cluster_barrier();  // every CTA of the rows runs
     const auto source = [&](int row) { return (const T*)a.x + (int64_t)row * a.ld + v0; };
     // where a row's results go, -1: nowhere
     const auto target = [&](int row) -> int64_t {
@@ -513,8 +510,7 @@ __global__ void __launch_bounds__(THREADS, topk_ctas<THREADS>()) k_topk(TopkArgs
                 if (a.rest && tid == 0) a.rest[to] = rest.z == 0.f ? -INFINITY : fmaf(rest.m, inv_tau, LN2 * lg2(rest.z));
             }
             // (the others' lists of the next row are to wait for these)
-            cluster_arrive();
-            cluster_wait();
+            cluster_barrier();
         }
         to = to1;
     }
