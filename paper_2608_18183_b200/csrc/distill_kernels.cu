@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
             };
             cp_async_wait_all();
             __syncwarp();
-            end_part(ss, p, PAD);
+            end_part(ss, p, -INFINITY);
             // they leave the row; v: their sums, student and teacher
             Pair v = Pair::none();
             bool any = false;
@@ -447,9 +447,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                 }
                 u.z = sum_of_warp(sum2(z));
             }
-            // (false too where the fill beside the row's ends would have a share: a row of values as low as it, a temperature so high)
-            const bool apart = (p.inner() == p.j0 && p.outer() == p.j1) || (u.m - to_f<TS>(from_f<TS>(PAD))) * c > 150.f;
-            if (!(u.z < 1e12f && u.z > 0.f && apart)) {
+            if (!(u.z < 1e12f && u.z > 0.f)) {
                 u = Mass::none();
                 for (int e = p.first() + lane; e < p.last(); e += 32) u.m = fmaxf(u.m, to_f<TS>(ss[e]));
                 u.share();
