@@ -322,14 +322,36 @@ __device__ __forceinline__ float softplus(float r) {
 struct ListCoefs {
     float Mx, My, Lx, Ly, kl_qp;  // logarithms and the divergence that the listed tokens' gradient needs
     float om, k0;                 // the others': 2^{(x - om) c} k0
-    int empty;
+    int empty, near;
+    float po, qo, ratio;          // the others' masses, and the logarithm of qo / po
 };
+
+// Divergences from lists below this are summed as terms none of which is negative, too: by the masses' logarithms the loss is off by up
+// to 2e-6, which is 3e-5 of it here.  (16384 rows of 16384 fp32 with lists of 64 345 us, all of them near 363.)
+constexpr float NEAR_LIST = 1.f / 16;
+
+// A warp's sum of such terms over the list's entries of a CTA, and of all others as one if asked for.
+__device__ __forceinline__ float near_list(const float* xk, const float* val, const int32_t* at, int k, float c, float inv_tau, float forward,
+                                           float reverse, const ListCoefs& f, bool others) {
+    const int lane = threadIdx.x & 31;
+    float2 sum = {0.f, 0.f};
+    if (others && lane == 0) sum = near_terms(f.po, f.qo, f.ratio);
+    for (int i = lane; i < k; i += 32)
+        if (at[i] >= 0) {
+            const float x = xk[i] - f.Mx, y = val[i] - f.My;
+            const float2 t = near_terms(ex2(fmaf(y, c, -f.Ly * LOG2E)), ex2(fmaf(x, c, -f.Lx * LOG2E)), (x - y) * inv_tau - (f.Lx - f.Ly));
+            sum.x += t.x;
+            sum.y += t.y;
+        }
+    return sum_of_warp((forward == 0.f ? 0.f : forward * sum.x) + (reverse == 0.f ? 0.f : reverse * sum.y));
+}
 
 template <typename TS, int THREADS, int PER_SM>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a) {
     constexpr int G = 16 / sizeof(TS), WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ ListCoefs coefs;
+    __shared__ float near_parts[ROW_CTAS];  // of a near row's loss, the first CTA's
     __shared__ int repeated[2];
     pdl_wait();
     pdl_trigger();
@@ -508,7 +530,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                     float k0 = a.forward * (ql + pl < qo + po ? pl - ql : qo - po);
                     if (a.reverse != 0.f && qo != 0.f) k0 += a.reverse * qo * (ratio - kl_qp);
                     k0 = u.z == 0.f ? 0.f : __fdividef(k0 * (w * inv_tau), u.z);
-                    coefs = {Mx, My, Lx, Ly, kl_qp, u.m == -INFINITY ? 0.f : u.m, k0, empty};
+                    const bool near = a.loss && !empty && (a.forward == 0.f || kl_pq < NEAR_LIST) && (a.reverse == 0.f || kl_qp < NEAR_LIST);
+                    coefs = {Mx, My, Lx, Ly, kl_qp, u.m == -INFINITY ? 0.f : u.m, k0, empty, near, po, qo, ratio};
                     if (a.loss && blockIdx.x % a.ctas == 0) {
                         float loss = 0.f;
                         if (!empty) {
@@ -522,12 +545,11 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
             if (w1 != 0.f) list(row + step, turn ^ 1, token, value);  // (the one before is used up; the others wait for one warp)
             __syncthreads();
             if (g) {
-                const ListCoefs f = coefs;
-                if (f.empty) {
+                if (coefs.empty) {
                     put_zeros(g, lo, hi);
                 } else {
                     const int Pg = phase_of(g);  // the gradient is written wide, whatever the others' alignment
-                    const f32x2 o = both(-f.om), c2 = both(c), K0 = both(f.k0);
+                    const f32x2 o = both(-coefs.om), c2 = both(c), K0 = both(coefs.k0);
                     const auto gradient = [&](float(&x)[G]) {
 #pragma unroll
                         for (int i = 0; i < G; i += 2) split(mul2(ex2(mul2(add2(both(x[i], x[i + 1]), o), c2)), K0), x[i], x[i + 1]);
@@ -567,6 +589,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                         }
                     }
                     __syncwarp();  // the listed tokens' places were written above
+                    const ListCoefs& f = coefs;
                     const float fw = w * inv_tau;
                     each([&](int i, int e) {
                         const float x = xk[i] - f.Mx, y = val[i] - f.My;
@@ -575,6 +598,21 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
                         if (a.reverse != 0.f && q != 0.f) d += a.reverse * q * ((x - y) * inv_tau - (f.Lx - f.Ly) - f.kl_qp);
                         g[e - p.P] = from_f<TS>(fw * d);
                     });
+                }
+            }
+            if (coefs.near) {  // (the same for all CTAs of the row, whose sums are the same bits)
+                if (threadIdx.x < 32) {
+                    const float loss = near_list(xk, val, at, k, c, inv_tau, a.forward, a.reverse, coefs, rank == 0);
+                    if (a.ctas > 1 && lane == 0) remote_store(remote_smem(near_parts + rank, 0), loss);
+                    if (a.ctas == 1 && lane == 0) a.loss[row] = loss;
+                }
+                if (a.ctas > 1) {
+                    cluster_barrier();
+                    if (rank == 0 && threadIdx.x == 0) {
+                        float loss = 0.f;
+                        for (int i = 0; i < a.ctas; ++i) loss += near_parts[i];
+                        a.loss[row] = loss;
+                    }
                 }
             }
             parity ^= 1;
@@ -623,7 +661,8 @@ cudaError_t run_distill(const DistillArgs& a, Stream& s) {
 template <typename TS>
 cudaError_t run_distill_topk(const DistillArgs& a, Stream& s) {
     return by_threads(a, 16 / sizeof(TS), 18, [&](auto threads) {
-        constexpr int THREADS = decltype(threads)::value, PER_SM = std::min(32, 1536 / THREADS);
+        // (48 registers: with the 40 that 1536 threads of an SM leave, 16384 rows of 16384 fp32 take 458 us in place of 345)
+        constexpr int THREADS = decltype(threads)::value, PER_SM = THREADS == 512 ? 2 : std::min(32, 1280 / THREADS);
         const size_t smem = (a.slice + 16) * sizeof(TS) + 2 * THREADS / 32 * a.ctas * (sizeof(Pair) + sizeof(Mass)) + a.k * 24 +
                             (a.slice + 31) / 32 * 4;
         int clusters = 0;
