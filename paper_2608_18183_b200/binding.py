@@ -183,7 +183,8 @@ def _rows(what, name, x, device=None, dtype=None, shape=None, written=False):
     global _torch, _types
     if _torch is None:
         import torch
-        _torch, _types = torch, {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+        _types = {torch.float32: DTYPE_FP32, torch.bfloat16: DTYPE_BF16}
+        _torch = torch  # (last: another thread that finds it uses the types)
     if not isinstance(x, _torch.Tensor) or not x.is_cuda:
         _refuse(what, f"{name} is not a tensor on a GPU")
     if device is not None and x.device != device:
