@@ -251,7 +251,7 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
                         history_row=None, history_len=None, repetition=1.0, frequency=0.0, presence=0.0, out=None,
                         stream=None):
     """Guidance, penalties, bias and masks on [rows, V] logits of fp32 or bf16 -> out, a new tensor or the given one (which may
-    be `logits`).  mask: int32 or uint32 words [masks, words], history: int32 [sequences, tokens], row numbers and
+    be `logits`, unless autograd needs those for a backward).  mask: int32 or uint32 words [masks, words], history: int32 [sequences, tokens], row numbers and
     lengths int32 [rows], bias fp32 [V]."""
     what = "hbsjd_adjust_logits"
     x, ld, dtype = _rows(what, "logits", logits)
@@ -290,11 +290,12 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
         sequences, cap = history.shape
         if not sequences or not cap:
             tok = None
-    if out is None:
+    given = out is not None
+    if given:
+        o, ld_out, _ = _rows(what, "out", out, device, logits.dtype, shape, written=True)
+    else:
         out = _torch.empty_like(logits, memory_format=_torch.contiguous_format)
         o, ld_out = out.data_ptr(), V
-    else:
-        o, ld_out, _ = _rows(what, "out", out, device, logits.dtype, shape, written=True)
     if rows == 0:
         return out
     d = hbsjd_adjust_desc(rows, V, dtype, masks, sequences, cap, ld, ld_u, ld_out, ld_mask, ld_history, cfg_scale, repetition,
@@ -303,6 +304,8 @@ def hbsjd_adjust_logits(logits, logits_u=None, cfg_scale=1.0, bias=None, mask=No
           _vector(what, "mask_row", mask_row, device, i32, rows), tok,
           _vector(what, "history_row", history_row, device, i32, rows),
           _vector(what, "history_len", history_len, device, i32, rows), o)
+    if given:
+        _torch.autograd.graph.increment_version(out)  # (autograd is to know that a saved tensor has changed)
     return out
 
 
@@ -331,7 +334,8 @@ def _distill(what, entry, logits_s, s, ld_s, dtype_s, teacher, dtype_t, ld_t, k,
     """What both forms of the divergence share: the gradient and the loss, and the call."""
     shape, device = logits_s.shape, logits_s.device
     rows, V = shape
-    if grad is not None:
+    given = grad is not None
+    if given:
         g, ld_g, _ = _rows(what, "grad", grad, device, logits_s.dtype, shape, written=True)
     elif want_grad:
         grad = _torch.empty_like(logits_s, memory_format=_torch.contiguous_format)
@@ -343,6 +347,8 @@ def _distill(what, entry, logits_s, s, ld_s, dtype_s, teacher, dtype_t, ld_t, k,
     if rows:
         d = hbsjd_distill_desc(rows, V, dtype_s, dtype_t, k, 0, ld_s, ld_t, ld_g, temperature, forward, reverse, 0)
         _call(what, entry, device, d, s, *teacher, w, loss.data_ptr(), g)
+        if given:
+            _torch.autograd.graph.increment_version(grad)
     return loss, grad
 
 
@@ -350,7 +356,8 @@ def hbsjd_distill(logits_s, logits_t, weight=None, temperature=1.0, forward=0.5,
                   stream=None):
     """forward KL(p || q) + reverse KL(q || p) of each row of the student's [rows, V] logits (q) against the teacher's (p), and
     weight times its gradient in logits_s: (loss fp32 [rows], grad like logits_s or None).  The defaults are Eq. 3.
-    grad: a tensor for the gradient, which may be logits_s.  In a training step: logits_s.backward(grad)."""
+    grad: a tensor for the gradient, which may be logits_s, unless autograd needs those for a backward (it refuses to go on then).  In a
+    training step: logits_s.backward(grad)."""
     what = "hbsjd_distill"
     s, ld_s, dtype_s = _rows(what, "logits_s", logits_s)
     device = logits_s.device
