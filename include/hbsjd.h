@@ -343,6 +343,7 @@ int hbsjd_score(hbsjd_ctx *student, hbsjd_ctx *teacher, int batch, const int32_t
  *   - Rows lie ld elements apart, any ld >= V (for what is only read: any ld >= 0; 0 is one row for all).  Pointers are
  *     aligned to their elements; rows that start on 16 bytes and arrays alike in that are fastest.
  *   - An array that is written may be one that is read (same pointer, stride and type); else they do not overlap.
+ *   - Temperatures are those for which log2(e) / temperature is a number: 4.3e-39 and above.
  *   - 1 <= V <= 131072, 0 <= rows < 2^27; rows = 0 does nothing.  Element types are HBSJD_DTYPE_*; arithmetic is fp32,
  *     bf16 results are rounded once.
  *   - A call gives the same bits every time.  The order of a row's sums depends on how the row is aligned and on how many rows

@@ -1253,7 +1253,7 @@ int score_topk(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32_t* pr
                float temperature, float* values, int32_t* indices, float* rest) {
     const int T = c->T, V = c->d.vocab;
     if (!tokens || !prefix_len || !class_labels || !values || !indices || batch < 1 || batch > c->Bmax || k < 1 || k > MAX_LISTED ||
-        k > V || !(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature)) {
+        k > V || !is_temperature(temperature)) {
         snprintf(c->err, sizeof(c->err), "hbsjd_score_topk: null argument, or batch %d, k %d or temperature %g out of range", batch, k,
                  temperature);
         return HBSJD_EINVAL;

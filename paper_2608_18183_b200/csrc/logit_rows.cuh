@@ -1,7 +1,7 @@
 // Rows of logits held in shared memory by one CTA or by a cluster of CTAs: staging of rows of any alignment, wide reads,
 // sums over the CTAs of a row, and the launch rules that the operators on rows share.
 #pragma once
-#include <math.h>
+#include <cmath>
 
 #include <algorithm>
 #include <atomic>
@@ -16,6 +16,9 @@ constexpr int ROW_CTAS = 8;            // CTAs of a row, at most (the portable c
 constexpr int ROW_SMEM = 216 * 1024;   // dynamic shared memory that a CTA may ask for
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
+
+// Exponents are taken in powers of two: x log2(e) / temperature.
+inline bool is_temperature(float t) { return t > 0.f && std::isfinite(t) && std::isfinite(LOG2E * (1.f / t)); }
 
 // 2^x.  Below 2^-126: zero.
 __device__ __forceinline__ float ex2(float x) {

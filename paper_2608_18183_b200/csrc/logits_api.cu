@@ -57,7 +57,7 @@ int distill_wrong(const char* what, const hbsjd_distill_desc* d, const void* s, 
     if (d->rows < 1 || d->rows > MAX_ROWS || d->V < 1 || d->V > MAX_LOGIT_V)
         return refuse("%s: %d rows of %d logits are out of range", what, d->rows, d->V);
     if (!is_dtype(d->dtype_s)) return refuse("%s: unknown type %d", what, d->dtype_s);
-    if (!(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature) ||
+    if (!is_temperature(d->temperature) ||
         !(d->forward >= 0.f) || !(d->reverse >= 0.f) || !std::isfinite(d->forward) || !std::isfinite(d->reverse))
         return refuse("%s: temperature %g or weights %g, %g are out of range", what, d->temperature, d->forward, d->reverse);
     if (!loss && !grad) return refuse("%s: neither loss nor gradient is asked for", what);
@@ -161,7 +161,7 @@ int hbsjd_topk_logits(void* cuda_stream, const hbsjd_topk_desc* d, const void* l
         return refuse("%s: %d rows of %d logits are out of range", what, d->rows, d->V);
     if (!is_dtype(d->dtype)) return refuse("%s: unknown type %d", what, d->dtype);
     if (d->k < 1 || d->k > MAX_LISTED || d->k > d->V) return refuse("%s: k = %d is out of range", what, d->k);
-    if (!(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature))
+    if (!is_temperature(d->temperature))
         return refuse("%s: temperature %g is out of range", what, d->temperature);
     if (const int rc = rows_wrong(what, "logits", logits, d->ld, d->V, elem(d->dtype), false)) return rc;
     if (!is_aligned(values, 4) || !is_aligned(indices, 4) || !is_aligned(rest, 4))
