@@ -614,7 +614,9 @@ class Context:
         batch, T = tokens.shape[0], self.shape.T
         assert tokens.is_cuda and tokens.dtype == torch.int32 and tokens.is_contiguous()
         assert tuple(tokens.shape) == (batch, T)
-        assert prefix_len.dtype == torch.int32 and class_labels.dtype == torch.int32
+        for x in (prefix_len, class_labels):  # (read through their pointers, one per image)
+            assert x.is_cuda and x.device == tokens.device and x.dtype == torch.int32 and x.is_contiguous()
+            assert len(x.shape) == 1 and x.shape[0] >= batch
         values = torch.empty((batch, T, k), dtype=torch.float32, device=tokens.device)
         indices = torch.empty((batch, T, k), dtype=torch.int32, device=tokens.device)
         rest = torch.empty((batch, T), dtype=torch.float32, device=tokens.device)
