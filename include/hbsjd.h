@@ -338,8 +338,9 @@ int hbsjd_score(hbsjd_ctx *student, hbsjd_ctx *teacher, int batch, const int32_t
  * What the distillation loop does with logits next to the rollout: rules in front of the sampler, the teacher's distribution
  * as a list of its largest logits, and divergences with their gradients (the score above is a value only).
  *   - They take no context: a stream (cudaStream_t as void*) of the current device, a descriptor and DEVICE pointers.
- *   - They launch one kernel and return; results are there when the stream has got that far.  They keep nothing between
- *     calls and allocate nothing: any number of calls may run at once, and a call may be captured into a CUDA graph.
+ *   - They launch one kernel and return; results are there when the stream has got that far.  They keep nothing of a call's
+ *     arrays (of a device, that a kernel's limits are set and how many clusters it holds) and allocate nothing: any number of
+ *     calls may run at once, and a call may be captured into a CUDA graph.
  *   - Rows lie ld elements apart, any ld >= V (for what is only read: any ld >= 0; 0 is one row for all).  Pointers are
  *     aligned to their elements; rows that start on 16 bytes and arrays alike in that are fastest.
  *   - An array that is written may be one that is read (same pointer, stride and type); else they do not overlap.
@@ -404,10 +405,11 @@ int hbsjd_score_topk(hbsjd_ctx *c, int batch, const int32_t *tokens, const int32
  *   weight   fp32 [rows] or NULL (all 1): a row's weight in the total, e.g. 1 / positions.  0 leaves the row out: it is not
  *            read, its loss is 0 and its gradient zeros
  *   loss     fp32 [rows] or NULL
- * An entry of -inf has no mass, neither has one whose share is below 2^-126.  Where the divergence is infinite (the student has
- * no mass where the teacher has: forward; the other way: reverse) so is the loss; the gradient of KL(p || q) is q - p all the
- * same, that of KL(q || p) is then not defined.  A row without mass on one side has loss 0 and gradient 0.  NaN and +inf
- * make the row's loss and gradient NaN.
+ * An entry of -inf has no mass, neither has one whose share is below 2^-126 (the type's lowest value beside any other).
+ * Where the divergence is infinite (the student has no mass where the teacher has: forward; the other way: reverse) so is the
+ * loss, or as large as a finite masking value makes it; the gradient of KL(p || q) is q - p all the same, that of KL(q || p)
+ * is then not defined.  A row without mass on one side has loss 0 and gradient 0.  NaN and +inf make the row's loss and
+ * gradient NaN.  A small loss has digits of its own: rows near one another are summed as terms none of which is negative.
  *
  * hbsjd_distill: p = softmax(logits_t / temperature), logits_t [rows, V] of type dtype_t.
  *

@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(THREADS) k_adjust(AdjustArgs a, int chunk, int
         __syncthreads();
         counts = table;
     }
-    const float inv = 1.f / a.repetition;
+    const float inv = 1.f / a.repetition;  // (a product with it has one rounding more than a division an entry, whose instructions bf16 rows have no room for)
     for (int e = e0; e < n;) {
 #pragma unroll
         for (int slot = 0; slot < AD_AHEAD; ++slot, e += STEP) {

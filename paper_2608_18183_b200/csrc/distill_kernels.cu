@@ -623,12 +623,12 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     }
 }
 
-// Threads of a CTA: 32 to 512, with at least `least` groups each if there are many rows.  What a warp does once a row is a good
-// part of its work, so that fewer warps are faster (16384 rows of 16384 fp32, lists of 64: 395 us with 256 threads, 439 with 512)
-// as long as other CTAs fill the SM; few rows have the SMs to themselves.
+// Threads of a CTA: as few, from 32 to 512, as have at most `most` groups each (four where there are few rows; 512 may have more).  What a
+// warp does once a row is a good part of its work, so that fewer warps are faster (16384 rows of 16384 fp32, lists of 64: 395 us with 256
+// threads, 439 with 512, both at 40 registers) as long as other CTAs fill the SM; few rows have the SMs to themselves.
 template <typename F>
-cudaError_t by_threads(const DistillArgs& a, int G, int least, F&& f) {
-    const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? least : 4) * G;
+cudaError_t by_threads(const DistillArgs& a, int G, int most, F&& f) {
+    const int per = ((int64_t)a.rows * a.ctas > device_sm_count() ? most : 4) * G;
     if (a.slice <= 32 * per) return f(std::integral_constant<int, 32>());
     if (a.slice <= 64 * per) return f(std::integral_constant<int, 64>());
     if (a.slice <= 128 * per) return f(std::integral_constant<int, 128>());
@@ -649,7 +649,8 @@ template <typename TS, typename TT>
 cudaError_t run_distill(const DistillArgs& a, Stream& s) {
     constexpr int G = sizeof(TS) == 2 && sizeof(TT) == 2 ? 8 : 4;
     return by_threads(a, G, 9, [&](auto threads) {
-        constexpr int THREADS = decltype(threads)::value, PER_SM = THREADS == 512 ? 2 : 768 / THREADS;  // (80 registers where there is room for three)
+        // (80 registers where there is room for three)
+        constexpr int THREADS = decltype(threads)::value, PER_SM = THREADS == 512 ? 2 : 768 / THREADS;
         const size_t smem = (a.slice + 16) * (sizeof(TS) + sizeof(TT)) + 2 * THREADS / 32 * a.ctas * sizeof(Pair);
         int clusters = 0;
         const cudaError_t e = deal<k_distill<TS, TT, THREADS, PER_SM>, THREADS, PER_SM>(a, smem, &clusters);

@@ -545,11 +545,15 @@ cudaError_t run_topk(TopkArgs& a, Stream& s) {
         if (e != cudaSuccess) return e;
         return launch_kc(true, k_topk<T, THREADS>, dim3((unsigned)clusters * a.ctas), dim3(THREADS), smem, s, a.ctas, a);
     };
-    // Many rows: eighteen groups a thread (256 threads for the largest slice), as for the divergences (lists of 64 from 8192 rows of
+    // Many rows: at most eighteen groups a thread (256 threads for the largest slice), as for the divergences (lists of 64 from 8192 rows of
     // 16384 fp32: 148 us with 256 threads, 185 with 512; from 16384 rows of 1000: 72 with one warp, 103 with four), and two
     // maxima per entry of the list.  Few rows: what is fastest for one (of 1000, lists of 64: 5 us with 256 threads, 7.6 with 64).
     const bool many = (int64_t)a.rows * a.ctas > device_sm_count();
-    const int per = (many ? 18 : 4) * G;
+    constexpr int MOST = 18;
+    const int per = (many ? MOST : 4) * G;
+    // (a thread marks its groups in the bits of a word; the row's place behind 16 bytes may take one more)
+    static_assert(MOST < 32 && ALONE_SM >= SHARED_SM && ALONE_SM / 16 + 2 <= 32 * 512 && MAX_LOGIT_V / ROW_CTAS / G + 2 <= 32 * 512,
+                  "512 threads have at most 32 groups each");
     if (many && a.slice <= 32 * per && a.k <= 64) return run(std::integral_constant<int, 32>());
     if (many && a.slice <= 64 * per && a.k <= 128) return run(std::integral_constant<int, 64>());
     if (many && a.slice <= 128 * per && a.k <= 256) return run(std::integral_constant<int, 128>());
