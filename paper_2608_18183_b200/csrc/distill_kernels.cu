@@ -221,12 +221,24 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
                 if (empty) {
                     put_zeros(g, lo, hi);
                 } else if (special[turn] || !(fabsf(v.ms) + fabsf(v.mt) + fabsf(k0) + fabsf(k1) + fabsf(k2) < 1e30f)) {
-                    // (the factors one by one: temperatures below 1e-15 leave none of their products)
-                    for (int e = lo + lane; e < hi; e += 32) {
-                        const float xo = to_f<TS>(ss[p.P + e]) - v.ms, yo = to_f<TT>(st[p.P + e]) - v.mt;
-                        const float q = ex2(fmaf(xo, c, -ls)), r = ex2(fmaf(yo, c, -lt));
-                        const float m = rev ? fmaf(a.reverse, (xo - yo - __fdividef(v.as, v.zs)) * inv_tau, a.forward) : a.forward;
-                        g[e] = from_f<TS>(fmaf(-a.forward, r, q == 0.f ? 0.f : q * m) * inv_tau * w);
+                    const auto each_entry = [&](auto&& slope) {
+                        for (int e = lo + lane; e < hi; e += 32) {
+                            const float xo = to_f<TS>(ss[p.P + e]) - v.ms, yo = to_f<TT>(st[p.P + e]) - v.mt;
+                            const float q = ex2(fmaf(xo, c, -ls)), r = ex2(fmaf(yo, c, -lt));
+                            g[e] = from_f<TS>(slope(q, r, xo - yo));
+                        }
+                    };
+                    if (fabsf(k0) + fabsf(k1) + fabsf(k2) < 1e30f) {
+                        each_entry([&](float q, float r, float d) {
+                            const float m = rev ? fmaf(k1, d, k0) : k0;
+                            return fmaf(-k2, r, q == 0.f ? 0.f : q * m);
+                        });
+                    } else {  // the factors one by one: temperatures below 1e-15 leave none of their products
+                        const float mean = __fdividef(v.as, v.zs);
+                        each_entry([&](float q, float r, float d) {
+                            const float m = rev ? fmaf(a.reverse, (d - mean) * inv_tau, a.forward) : a.forward;
+                            return fmaf(-a.forward, r, q == 0.f ? 0.f : q * m) * inv_tau * w;
+                        });
                     }
                 } else {
                     // At an entry of the type's lowest value d is about that, and finite, since both references are far less; but k1 above 1
