@@ -8,8 +8,9 @@
 // (two fp32 rows) are what bounds the kernel.  Rows are dealt to resident CTAs.  A warp has a part of the row to itself: it stages
 // it, sums over it and writes its gradient, waits for the others for the sums alone, and fetches its part of the next row when it
 // is done with its own.  Long rows are split over a cluster, whose CTAs exchange the sums through distributed shared memory; so are
-// few rows, to use more SMs.  Measured: 8192 pairs of rows of 16384 fp32 272 us (0.82 of a copy's rate, a cluster of two a row), 16384
-// rows against lists of 64 388 us (0.79), both with gradients; 8192 pairs in bf16 184 us, where the four exponentials an entry take 119.
+// few rows, to use more SMs.  Measured, the kernel alone: 8192 pairs of rows of 16384 fp32 277 us (0.81 of a copy's rate, a cluster of two
+// a row), 16384 rows against lists of 64 345 us (0.89), both with gradients; 8192 pairs in bf16 184 us, where the four exponentials an entry
+// take 119.
 #include <type_traits>
 
 #include "logit_rows.cuh"
