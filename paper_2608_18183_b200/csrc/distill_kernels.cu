@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
     __shared__ int special[3];  // a logit of the slice asks for care: this row, the one before, the one behind
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const int rank = blockIdx.x % a.ctas, v0 = rank * a.slice, n = max(0, min(a.slice, a.V - v0));
     const int step = gridDim.x / a.ctas;
     const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
     const auto fetch = [&](int row) {
         const TS* s = (const TS*)a.s + (int64_t)row * a.ld_s + v0;
         const TT* t = (const TT*)a.t + (int64_t)row * a.ld_t + v0;
-        const Part<G, WARPS> p(common_phase(s, t), n);
+        const Part<G, WARPS> p(common_phase(s, t), n, wid);
         stage_part(ss, s, p);
         stage_part(st, t, p);
     };
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill(DistillArgs a) {
         const float w2 = weight(row + 2 * step);  // (so that no fetch waits for a weight)
         bool fetched = w1 == 0.f;
         TS* g = a.grad ? (TS*)a.grad + (int64_t)row * a.ld_g + v0 : nullptr;
-        const Part<G, WARPS> p(common_phase((const TS*)a.s + (int64_t)row * a.ld_s + v0, (const TT*)a.t + (int64_t)row * a.ld_t + v0), n);
+        const Part<G, WARPS> p(common_phase((const TS*)a.s + (int64_t)row * a.ld_s + v0, (const TT*)a.t + (int64_t)row * a.ld_t + v0), n, wid);
         const int lo = p.first() - p.P, hi = p.last() - p.P;  // the warp's entries of the slice
         if (w == 0.f) {                                       // (all CTAs of the row)
             if (g) put_zeros(g, lo, hi);
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     __shared__ int repeated[2];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, k = a.k;
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, k = a.k;
     const int rank = blockIdx.x % a.ctas, v0 = rank * a.slice, n = max(0, min(a.slice, a.V - v0));
     const int step = gridDim.x / a.ctas, places = WARPS * a.ctas;
     const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
     const auto weight = [&](int row) { return row >= a.rows ? 0.f : a.weight ? __ldg(a.weight + row) : 1.f; };
     const auto fetch = [&](int row) {
         const TS* s = (const TS*)a.s + (int64_t)row * a.ld_s + v0;
-        stage_part(ss, s, Part<G, WARPS>(phase_of(s), n));
+        stage_part(ss, s, Part<G, WARPS>(phase_of(s), n, wid));
     };
     // A row's list, one entry a thread (the last warps first: warp 0 has other work): those of the slice find their places.
     const int first = THREADS - 1 - threadIdx.x;
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_distill_topk(DistillArgs a)
             value = __ldg(a.values + (int64_t)(row + step) * k + first);
         }
         TS* g = a.grad ? (TS*)a.grad + (int64_t)row * a.ld_g + v0 : nullptr;
-        const Part<G, WARPS> p(phase_of((const TS*)a.s + (int64_t)row * a.ld_s + v0), n);
+        const Part<G, WARPS> p(phase_of((const TS*)a.s + (int64_t)row * a.ld_s + v0), n, wid);
         const int lo = p.first() - p.P, hi = p.last() - p.P;  // the warp's entries of the slice
         if (w == 0.f) {                                       // (all CTAs of the row)
             if (g) put_zeros(g, lo, hi);

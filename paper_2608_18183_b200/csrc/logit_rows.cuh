@@ -7,6 +7,7 @@
 #include <atomic>
 
 #include "internal.h"
+#include "row_parts.cuh"
 
 namespace hbsjd {
 
@@ -226,25 +227,7 @@ __device__ __forceinline__ void put_at(T* out, int i, int lo, int hi, const floa
     }
 }
 
-// ------------------------------------------------------------------ a warp's part of a row
-// A slice of n elements, the first of them P elements behind a 16-byte boundary in shared memory, as groups of G; a warp has the
-// groups [j0, j1) to itself.  It stages them, sums over them and writes their gradient without waiting for other warps.
-template <int G, int WARPS>
-struct Part {
-    int P, n, j0, j1;
-    __device__ __forceinline__ Part(int P, int n) : P(P), n(n) {
-        const int groups = (P + n + G - 1) / G, each = ((groups + WARPS - 1) / WARPS + 1) / 2 * 2;  // (even: 16 bytes of bf16)
-        j0 = min((int)(threadIdx.x >> 5) * each, groups);
-        j1 = min(j0 + each, groups);
-    }
-    // groups [inner(), outer()) are the row's in whole
-    __device__ __forceinline__ int inner() const { return j0 * G >= P ? j0 : min((P + G - 1) / G, j1); }
-    __device__ __forceinline__ int outer() const { return max(min(j1, (P + n) / G), inner()); }
-    // staged elements [first(), last()) are the row's, in it from element first() - P on
-    __device__ __forceinline__ int first() const { return max(j0 * G, P); }
-    __device__ __forceinline__ int last() const { return min(j1 * G, P + n); }
-};
-
+// ------------------------------------------------------------------ a warp's part of a row (see row_parts.cuh)
 // The words of the less than 16 bytes in front of the part's whole vectors, and of those behind.
 template <typename T, int G, int WARPS>
 __device__ __forceinline__ void stage_ends(T* dst, const T* src, const Part<G, WARPS>& p) {
