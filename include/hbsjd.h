@@ -405,7 +405,8 @@ int hbsjd_score_topk(hbsjd_ctx *c, int batch, const int32_t *tokens, const int32
  *   weight   fp32 [rows] or NULL (all 1): a row's weight in the total, e.g. 1 / positions.  0 leaves the row out: it is not
  *            read, its loss is 0 and its gradient zeros
  *   loss     fp32 [rows] or NULL
- * An entry of -inf has no mass, neither has one whose share is below 2^-126 (the type's lowest value beside any other).
+ * An entry of -inf has no mass, neither has one of 88 temperatures and more below the row's largest (the type's lowest value
+ * beside any other); between a share of 2^-126 and that it may count or not.
  * Where the divergence is infinite (the student has no mass where the teacher has: forward; the other way: reverse) so is the
  * loss, or as large as a finite masking value makes it; the gradient of KL(p || q) is q - p all the same, that of KL(q || p)
  * is then not defined.  A row without mass on one side has loss 0 and gradient 0.  NaN and +inf make the row's loss and
