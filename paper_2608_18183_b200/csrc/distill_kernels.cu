@@ -8,8 +8,8 @@
 // (two fp32 rows) are what bounds the kernel.  Rows are dealt to resident CTAs.  A warp has a part of the row to itself: it stages
 // it, sums over it and writes its gradient, waits for the others for the sums alone, and fetches its part of the next row when it
 // is done with its own.  Long rows are split over a cluster, whose CTAs exchange the sums through distributed shared memory; so are
-// few rows, to use more SMs.  Measured, the kernel alone: 8192 pairs of rows of 16384 fp32 277 us (0.81 of a copy's rate, a cluster of two
-// a row), 16384 rows against lists of 64 345 us (0.89), both with gradients; 8192 pairs in bf16 184 us, where the four exponentials an entry
+// few rows, to use more SMs.  Measured, the kernel alone: 8192 pairs of rows of 16384 fp32 278 us (0.81 of a copy's rate, a cluster of two
+// a row), 16384 rows against lists of 64 340 us (0.91), both with gradients; 8192 pairs in bf16 184 us, where the four exponentials an entry
 // take 119.
 #include <type_traits>
 
@@ -29,7 +29,7 @@ __device__ __forceinline__ int common_phase(const TS* s, const TT* t) {
 
 // Divergences below this are summed as terms none of which is negative.  As delta - E_p d the loss is off by what two sums' quotient and
 // its logarithm are, up to 7e-7 whatever the divergence is: 5e-5 of it here, more than all of a KL of 5e-7 (7e-5 of that as these terms).
-// Such rows cost a third look: 8192 pairs of 16384 fp32 with gradients 374 us in place of 278, bf16 291 in place of 185.
+// Such rows cost a third look: 8192 pairs of 16384 fp32 with gradients 375 us in place of 278, bf16 290 in place of 184.
 constexpr float NEAR = 1.f / 64;
 
 // An outcome's p (e^r - 1 - r) and q (e^-r - 1 + r), r = log q / p, of any size: those far from one another as they are; no mass on either
@@ -340,7 +340,7 @@ struct ListCoefs {
 };
 
 // Divergences from lists below this are summed as terms none of which is negative, too: by the masses' logarithms the loss is off by up
-// to 2e-6, which is 3e-5 of it here.  (16384 rows of 16384 fp32 with lists of 64 345 us, all of them near 363.)
+// to 2e-6, which is 3e-5 of it here.  (16384 rows of 16384 fp32 with lists of 64 340 us, all of them near 356.)
 constexpr float NEAR_LIST = 1.f / 16;
 
 // A warp's sum of such terms over the list's entries of a CTA, and of all others as one if asked for.
