@@ -430,6 +430,98 @@ int hbsjd_distill(void *cuda_stream, const hbsjd_distill_desc *d, const void *lo
 int hbsjd_distill_topk(void *cuda_stream, const hbsjd_distill_desc *d, const void *logits_s, const float *values,
                        const int32_t *indices, const float *rest, const float *weight, float *loss, void *grad);
 
+/* ---- training by rewards and preferences -----------------------------------------------------------------------------------
+ * The on-policy step without a teacher: log-probabilities of the sampled tokens, losses on them with their gradients, and the
+ * clipping of the gradients that they end in.  The conventions are those of the operators on rows of logits, with x = logits /
+ * temperature and q = softmax(x); tokens are int32 [rows], and one outside 0..V-1 leaves its row out: it is not read, its outputs are
+ * 0 and its gradient zeros.  An entry of -inf has no mass; NaN and +inf make what their row gives NaN.
+ *
+ * hbsjd_token_logprobs: logp[r] = log q_token (-inf: no mass), entropy[r] = -sum q log q;  fp32 [rows], either may be NULL.  A row
+ *   without mass: -inf and 0.
+ * hbsjd_token_logprobs_grad: grad[r] = d (d_logp[r] logp[r] + d_entropy[r] entropy[r]) / d logits[r], what a loss of the caller's
+ *   own gives back; d_logp, d_entropy fp32 [rows], d_entropy may be NULL.  Rows where both are 0 are left out. */
+typedef struct {
+    int32_t rows, V, dtype, reserved;
+    int64_t ld, ld_grad;
+    float temperature;
+    uint32_t reserved2;
+} hbsjd_token_desc;
+int hbsjd_token_logprobs(void *cuda_stream, const hbsjd_token_desc *d, const void *logits, const int32_t *tokens, float *logp,
+                         float *entropy);
+int hbsjd_token_logprobs_grad(void *cuda_stream, const hbsjd_token_desc *d, const void *logits, const int32_t *tokens,
+                              const float *d_logp, const float *d_entropy, void *grad);
+
+/* hbsjd_token_logprobs of a model's own distributions over completed trajectories, at 8 bytes a position in place of 4 V: the old
+ * policy's and the reference's sides of the losses below.  The model of context c runs the forwards of hbsjd_score; entry
+ * [b, t - 1] of the outputs is of token x_t given x_<t, 0 for the positions t <= prefix_len[b].
+ *   tokens DEVICE int32 [batch, T], prefix_len, class_labels DEVICE int32 [batch]: as hbsjd_score
+ *   logp, entropy DEVICE fp32 [batch, T], entropy may be NULL
+ * Runs on the context's stream and waits; its rollout state and KV caches are overwritten.  Errors as hbsjd_score. */
+int hbsjd_score_logprobs(hbsjd_ctx *c, int batch, const int32_t *tokens, const int32_t *prefix_len, const int32_t *class_labels,
+                         float temperature, float *logp, float *entropy);
+
+/* The clipped policy loss of every row and its gradient.  With l = log q_token, r = e^{l - old_logp}, A = advantage, d = ref_logp - l:
+ *   loss[r] = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)      (A < 0 and dual_clip > 0: at most -dual_clip A)
+ *             + kl (e^d - 1 - d) - entropy H;                         grad[r] = weight[r] d loss[r] / d logits[r]
+ *   advantage fp32 [rows];  old_logp fp32 [rows] or NULL: l itself, the ratio is 1;  ref_logp fp32 [rows], NULL where kl = 0
+ *   weight    fp32 [rows] or NULL (all 1): as hbsjd_distill; 0 leaves the row out
+ *   loss, logp, entropy_out  fp32 [rows] or NULL;  grad [rows, V] of type dtype, or NULL
+ * Where the ratio is clipped, its slope is 0.  A row without mass has loss 0 and gradient 0.  Of a token without mass the ratio is 0 (1
+ * where old_logp is -inf, too); with a KL term against a finite ref_logp its loss is +inf, and its gradient not defined.
+ * 0 <= clip_low <= 1, clip_high >= 0, dual_clip = 0 (none) or > 1, kl >= 0, entropy any finite number. */
+typedef struct {
+    int32_t rows, V, dtype, reserved;
+    int64_t ld, ld_grad;
+    float temperature, clip_low, clip_high, dual_clip, kl, entropy;
+} hbsjd_policy_desc;
+int hbsjd_policy_loss(void *cuda_stream, const hbsjd_policy_desc *d, const void *logits, const int32_t *tokens,
+                      const float *advantage, const float *old_logp, const float *ref_logp, const float *weight, float *loss,
+                      float *logp, float *entropy_out, void *grad);
+
+/* A loss of pairs of sequences, one preferred to the other, and its gradient.  Sequence s is rows offsets[s] .. offsets[s + 1] - 1;
+ *   S_s = sum over its rows of weight[r] (log q_token - ref_logp[r]),   h = S_chosen - S_rejected:
+ *   HBSJD_PREFERENCE_SIGMOID  z = beta h - margin,  loss = -(1 - smoothing) log sigmoid(z) - smoothing log sigmoid(-z)
+ *   HBSJD_PREFERENCE_HINGE    the same z,           loss = max(0, 1 - z)
+ *   HBSJD_PREFERENCE_SQUARE   loss = (h - 1 / (2 beta))^2
+ *   grad[r] = d (sum over pairs of pair_weight loss) / d logits[r]
+ * Pair p is sequences 2 p (chosen) and 2 p + 1 where `interleaved`, else p (chosen) and pairs + p.
+ *   offsets   int32 [2 pairs + 1], not decreasing, within 0..rows; else all losses, sums and gradients are NaN
+ *   ref_logp  fp32 [rows] or NULL (0);  weight fp32 [rows] or NULL (all 1): 0 leaves a row out;  pair_weight fp32 [pairs] or NULL
+ *   loss fp32 [pairs] or NULL;  sums fp32 [2 pairs] or NULL: S_s;  logp fp32 [rows] or NULL: log q_token (0: left out)
+ *   grad [rows, V] or NULL: zeros for rows of no sequence
+ *   workspace hbsjd_preference_workspace(d) bytes, aligned to 16, which no other call uses at the same time; whatever it holds
+ * smoothing in 0..1 and margin are 0 where the loss has none; beta > 0.  Launches several kernels. */
+enum { HBSJD_PREFERENCE_SIGMOID = 0, HBSJD_PREFERENCE_HINGE = 1, HBSJD_PREFERENCE_SQUARE = 2 };
+typedef struct {
+    int32_t rows, V, dtype, pairs, kind, interleaved;
+    int64_t ld, ld_grad;
+    float temperature, beta, smoothing, margin;
+} hbsjd_preference_desc;
+size_t hbsjd_preference_workspace(const hbsjd_preference_desc *d);
+int hbsjd_preference_loss(void *cuda_stream, const hbsjd_preference_desc *d, const void *logits, const int32_t *tokens,
+                          const int32_t *offsets, const float *ref_logp, const float *weight, const float *pair_weight,
+                          void *workspace, float *loss, float *sums, float *logp, void *grad);
+
+/* The norm of all gradients as one vector, and their scaling by min(1, max_norm / (norm + 1e-6)).
+ *   gradients, out, sizes, dtypes  HOST arrays [count]: DEVICE pointers to dense arrays of sizes[i] elements of type dtypes[i], which
+ *             may be dropped when the call returns.  out NULL or out[i] = gradients[i]: in place, else out[i] gets the scaled ones, or
+ *             copies where nothing is scaled; all of them or none.  No two arrays may overlap.
+ *   norm      DEVICE fp32: before scaling.  HBSJD_NORM_2: root of the sum of squares, summed so that neither large nor small
+ *             gradients leave the type's range on the way; HBSJD_NORM_MAX: the largest magnitude
+ *   max_norm  >= 0; +inf: the norm alone.  Where the norm is infinite or NaN nothing is scaled, and the norm says so
+ *   workspace hbsjd_clip_workspace(count) bytes, aligned to 16, which no other call uses at the same time; whatever it holds
+ * 0 <= count <= 2^20.  The parameters of its kernels hold the pointers, so a captured call keeps them.  Launches two kernels (two
+ * for each 1024 arrays beyond 128). */
+enum { HBSJD_NORM_2 = 0, HBSJD_NORM_MAX = 1 };
+typedef struct {
+    int32_t count, norm;
+    float max_norm;
+    uint32_t reserved;
+} hbsjd_clip_desc;
+size_t hbsjd_clip_workspace(int count);
+int hbsjd_clip_gradients(void *cuda_stream, const hbsjd_clip_desc *d, const void *const *gradients, void *const *out,
+                         const int64_t *sizes, const int32_t *dtypes, void *workspace, float *norm);
+
 /* Per-kernel-class timing with CUDA events on the context's stream (off by default).  While enabled,
  * every launch of a timed class is bracketed by an event pair; totals accumulate until the next
  * hbsjd_profile(c, 1), which also resets them.  work = algorithmic FLOPs (GEMM: 2 M N K per launch) or

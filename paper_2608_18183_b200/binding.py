@@ -22,7 +22,8 @@ EXPORTS = ["hbsjd_create", "hbsjd_rollout", "hbsjd_prefill_passes", "hbsjd_rollo
            "hbsjd_debug_shuffle_pages", "hbsjd_debug_fold_norm", "hbsjd_debug_fail_round",
            "hbsjd_debug_force_tile", "hbsjd_gemm", "hbsjd_bikl", "hbsjd_score", "hbsjd_strerror",
            "hbsjd_last_error", "hbsjd_adjust_logits", "hbsjd_topk_logits", "hbsjd_distill", "hbsjd_distill_topk",
-           "hbsjd_score_topk"]
+           "hbsjd_score_topk", "hbsjd_token_logprobs", "hbsjd_token_logprobs_grad", "hbsjd_score_logprobs", "hbsjd_policy_loss",
+           "hbsjd_preference_workspace", "hbsjd_preference_loss", "hbsjd_clip_workspace", "hbsjd_clip_gradients"]
 
 
 class hbsjd_model_desc(C.Structure):
@@ -81,6 +82,25 @@ class hbsjd_distill_desc(C.Structure):
             (n, C.c_float) for n in ("temperature", "forward", "reverse")] + [("reserved2", C.c_uint32)]
 
 
+class hbsjd_token_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "V", "dtype", "reserved")] + [(n, C.c_int64) for n in ("ld", "ld_grad")] + [
+        ("temperature", C.c_float), ("reserved2", C.c_uint32)]
+
+
+class hbsjd_policy_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "V", "dtype", "reserved")] + [(n, C.c_int64) for n in ("ld", "ld_grad")] + [
+        (n, C.c_float) for n in ("temperature", "clip_low", "clip_high", "dual_clip", "kl", "entropy")]
+
+
+class hbsjd_preference_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "V", "dtype", "pairs", "kind", "interleaved")] + [
+        (n, C.c_int64) for n in ("ld", "ld_grad")] + [(n, C.c_float) for n in ("temperature", "beta", "smoothing", "margin")]
+
+
+class hbsjd_clip_desc(C.Structure):
+    _fields_ = [("count", C.c_int32), ("norm", C.c_int32), ("max_norm", C.c_float), ("reserved", C.c_uint32)]
+
+
 class HbsjdError(RuntimeError):
     def __init__(self, code, what, detail=""):
         super().__init__(f"{what}: {code} ({detail})")
@@ -136,6 +156,16 @@ def load():
         L.hbsjd_distill.argtypes = [vp, C.POINTER(hbsjd_distill_desc)] + [vp] * 5
         L.hbsjd_distill_topk.argtypes = [vp, C.POINTER(hbsjd_distill_desc)] + [vp] * 7
         L.hbsjd_score_topk.argtypes = [vp, C.c_int, vp, vp, vp, C.c_int, C.c_float, vp, vp, vp]
+        L.hbsjd_token_logprobs.argtypes = [vp, C.POINTER(hbsjd_token_desc)] + [vp] * 4
+        L.hbsjd_token_logprobs_grad.argtypes = [vp, C.POINTER(hbsjd_token_desc)] + [vp] * 5
+        L.hbsjd_score_logprobs.argtypes = [vp, C.c_int, vp, vp, vp, C.c_float, vp, vp]
+        L.hbsjd_policy_loss.argtypes = [vp, C.POINTER(hbsjd_policy_desc)] + [vp] * 10
+        L.hbsjd_preference_workspace.argtypes = [C.POINTER(hbsjd_preference_desc)]
+        L.hbsjd_preference_workspace.restype = C.c_size_t
+        L.hbsjd_preference_loss.argtypes = [vp, C.POINTER(hbsjd_preference_desc)] + [vp] * 11
+        L.hbsjd_clip_workspace.argtypes = [C.c_int]
+        L.hbsjd_clip_workspace.restype = C.c_size_t
+        L.hbsjd_clip_gradients.argtypes = [vp, C.POINTER(hbsjd_clip_desc)] + [vp] * 6
         L.hbsjd_strerror.argtypes = [C.c_int]
         L.hbsjd_strerror.restype = C.c_char_p
         L.hbsjd_last_error.argtypes = [vp]
@@ -388,6 +418,207 @@ def hbsjd_distill_topk(logits_s, values, indices, rest=None, weight=None, temper
                     0, 0, values.shape[1], weight, temperature, forward, reverse, want_grad, grad)
 
 
+# ---- training by rewards and preferences (see include/hbsjd.h)
+
+PREFERENCE = {"sigmoid": 0, "hinge": 1, "square": 2}
+NORM = {"2": 0, "max": 1}
+
+
+def _gradient(what, grad, want, logits):
+    """(tensor, pointer, row stride) of the gradient: the given tensor, a new one, or none."""
+    if grad is not None:
+        return (grad, *_rows(what, "grad", grad, logits.device, logits.dtype, logits.shape, written=True)[:2])
+    if not want:
+        return None, None, 0
+    grad = _torch.empty_like(logits, memory_format=_torch.contiguous_format)
+    return grad, grad.data_ptr(), logits.shape[1]
+
+
+def _tokens(what, tokens, device, rows):
+    if tokens is None:
+        _refuse(what, "tokens are missing")
+    return _vector(what, "tokens", tokens, device, _torch.int32, rows)
+
+
+def hbsjd_token_logprobs(logits, tokens, temperature=1.0, want_entropy=True, stream=None):
+    """Log-probability of each row's token under softmax(logits / temperature) and the entropy of that distribution: (logp fp32
+    [rows], entropy fp32 [rows] or None).  logits [rows, V] of fp32 or bf16, tokens int32 [rows]; a token outside 0..V-1 leaves its row
+    out (0, 0)."""
+    what = "hbsjd_token_logprobs"
+    x, ld, dtype = _rows(what, "logits", logits)
+    device = logits.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_token_logprobs, what, logits, stream, (logits, tokens, temperature, want_entropy), {})
+    rows, V = logits.shape
+    t = _tokens(what, tokens, device, rows)
+    logp = logits.new_empty((rows,), dtype=_torch.float32)
+    entropy = _torch.empty_like(logp) if want_entropy else None
+    if rows:
+        _call(what, load().hbsjd_token_logprobs, device, hbsjd_token_desc(rows, V, dtype, 0, ld, 0, temperature, 0), x, t,
+              logp.data_ptr(), entropy.data_ptr() if want_entropy else None)
+    return logp, entropy
+
+
+def hbsjd_token_logprobs_grad(logits, tokens, d_logp, d_entropy=None, temperature=1.0, grad=None, stream=None):
+    """The backward of hbsjd_token_logprobs: from a loss's derivatives in logp and entropy (fp32 [rows]; the second may be None) its
+    gradient in the logits, a new tensor or the given one (which may be `logits`, unless autograd needs those for a backward)."""
+    what = "hbsjd_token_logprobs_grad"
+    x, ld, dtype = _rows(what, "logits", logits)
+    device = logits.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_token_logprobs_grad, what, logits, stream, (logits, tokens, d_logp, d_entropy, temperature, grad), {})
+    rows, V = logits.shape
+    t, f32 = _tokens(what, tokens, device, rows), _torch.float32
+    if d_logp is None:
+        _refuse(what, "d_logp is missing")
+    a, b = _vector(what, "d_logp", d_logp, device, f32, rows), _vector(what, "d_entropy", d_entropy, device, f32, rows)
+    given = grad is not None
+    grad, g, ld_g = _gradient(what, grad, True, logits)
+    if rows:
+        _call(what, load().hbsjd_token_logprobs_grad, device, hbsjd_token_desc(rows, V, dtype, 0, ld, ld_g, temperature, 0), x, t, a, b, g)
+        if given:
+            _torch.autograd.graph.increment_version(grad)
+    return grad
+
+
+def hbsjd_policy_loss(logits, tokens, advantage, old_logp=None, ref_logp=None, weight=None, temperature=1.0, clip_low=0.2,
+                      clip_high=0.2, dual_clip=0.0, kl=0.0, entropy=0.0, want_grad=True, want_entropy=False, grad=None, stream=None):
+    """The clipped policy loss of each row, with `kl` times the KL estimate e^d - 1 - d against the reference (d = ref_logp - logp) and
+    less `entropy` times the entropy, and weight times its gradient in the logits: (loss fp32 [rows], grad like logits or None, logp
+    fp32 [rows], entropy fp32 [rows] or None).  advantage, old_logp (None: the ratio is one), ref_logp (None where kl is 0) and weight
+    (None: ones; 0 leaves a row out) fp32 [rows].  grad: as in hbsjd_distill.  In a training step: logits.backward(grad)."""
+    what = "hbsjd_policy_loss"
+    x, ld, dtype = _rows(what, "logits", logits)
+    device = logits.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_policy_loss, what, logits, stream,
+                          (logits, tokens, advantage, old_logp, ref_logp, weight, temperature, clip_low, clip_high, dual_clip, kl, entropy,
+                           want_grad, want_entropy, grad), {})
+    rows, V = logits.shape
+    t, f32 = _tokens(what, tokens, device, rows), _torch.float32
+    if advantage is None:
+        _refuse(what, "advantage is missing")
+    row = [_vector(what, name, v, device, f32, rows) for name, v in (
+        ("advantage", advantage), ("old_logp", old_logp), ("ref_logp", ref_logp), ("weight", weight))]
+    given = grad is not None
+    grad, g, ld_g = _gradient(what, grad, want_grad, logits)
+    loss = logits.new_empty((rows,), dtype=f32)
+    logp = _torch.empty_like(loss)
+    H = _torch.empty_like(loss) if want_entropy else None
+    if rows:
+        d = hbsjd_policy_desc(rows, V, dtype, 0, ld, ld_g, temperature, clip_low, clip_high, dual_clip, kl, entropy)
+        _call(what, load().hbsjd_policy_loss, device, d, x, t, *row, loss.data_ptr(), logp.data_ptr(),
+              H.data_ptr() if want_entropy else None, g)
+        if given:
+            _torch.autograd.graph.increment_version(grad)
+    return loss, grad, logp, H
+
+
+def hbsjd_preference_loss(logits, tokens, offsets, ref_logp=None, weight=None, pair_weight=None, temperature=1.0, beta=0.1,
+                          kind="sigmoid", smoothing=0.0, margin=0.0, interleaved=False, want_grad=True, grad=None, stream=None):
+    """The loss of pairs of sequences, one preferred to the other, and its gradient in the logits: (loss fp32 [pairs], grad like
+    logits or None, sums fp32 [2 pairs]: weight (logp - ref_logp) summed over each sequence).  Sequence s is rows offsets[s] ..
+    offsets[s + 1] - 1 (int32 [2 pairs + 1]); the chosen ones are the even ones if interleaved, else the first half.  ref_logp, weight
+    fp32 [rows], pair_weight fp32 [pairs] or None.  kind: "sigmoid", "hinge" or "square" (see include/hbsjd.h).  grad: as in
+    hbsjd_distill."""
+    what = "hbsjd_preference_loss"
+    x, ld, dtype = _rows(what, "logits", logits)
+    device = logits.device
+    if stream is not None or device.index != _torch.cuda.current_device():
+        return _elsewhere(hbsjd_preference_loss, what, logits, stream,
+                          (logits, tokens, offsets, ref_logp, weight, pair_weight, temperature, beta, kind, smoothing, margin, interleaved,
+                           want_grad, grad), {})
+    rows, V = logits.shape
+    t, f32 = _tokens(what, tokens, device, rows), _torch.float32
+    if kind not in PREFERENCE:
+        _refuse(what, f"unknown loss {kind!r}")
+    count = offsets.shape[0] if isinstance(offsets, _torch.Tensor) and offsets.dim() == 1 else 0
+    if count < 3 or count % 2 == 0:
+        _refuse(what, "offsets are to be a vector of 2 pairs + 1")
+    pairs = count // 2
+    at = _vector(what, "offsets", offsets, device, _torch.int32, count)
+    ref, w = _vector(what, "ref_logp", ref_logp, device, f32, rows), _vector(what, "weight", weight, device, f32, rows)
+    pw = _vector(what, "pair_weight", pair_weight, device, f32, pairs)
+    given = grad is not None
+    grad, g, ld_g = _gradient(what, grad, want_grad, logits)
+    out = logits.new_empty((3 * pairs,), dtype=f32)
+    loss, sums = out[:pairs], out[pairs:]
+    if not rows:
+        _refuse(what, "sequences without a row")
+    d = hbsjd_preference_desc(rows, V, dtype, pairs, PREFERENCE[kind], 1 if interleaved else 0, ld, ld_g, temperature, beta, smoothing,
+                              margin)
+    L = load()
+    work = logits.new_empty((L.hbsjd_preference_workspace(d),), dtype=_torch.uint8)
+    _call(what, L.hbsjd_preference_loss, device, d, x, t, at, ref, w, pw, work.data_ptr(), loss.data_ptr(), sums.data_ptr(), None, g)
+    if given:
+        _torch.autograd.graph.increment_version(grad)
+    return loss, grad, sums
+
+
+def _dense(x):
+    """Whether x's elements fill one stretch of memory, in any order."""
+    if x.is_contiguous():
+        return True
+    size = 1
+    for step, n in sorted((s, n) for s, n in zip(x.stride(), x.shape) if n != 1):
+        if step != size:
+            return False
+        size *= n
+    return True
+
+
+def hbsjd_clip_gradients(gradients, max_norm=float("inf"), norm="2", out=None, stream=None):
+    """The norm of all gradients (a list of dense fp32 or bf16 tensors on one GPU) as one vector, a new fp32 scalar on that GPU; they are
+    scaled in place by min(1, max_norm / (norm + 1e-6)), or into `out`, tensors like them, which get copies where nothing is scaled.
+    norm: "2" or "max" (the largest magnitude).  An infinite or NaN norm scales nothing.  max_norm = inf: the norm alone.  No two
+    tensors may overlap."""
+    what = "hbsjd_clip_gradients"
+    gradients = list(gradients)
+    if not gradients:
+        _refuse(what, "no gradients")
+    if _torch is None:
+        try:
+            _rows(what, "gradients", None)  # (finds torch)
+        except HbsjdError:
+            pass
+    if not isinstance(gradients[0], _torch.Tensor) or not gradients[0].is_cuda:
+        _refuse(what, "gradients[0] is not a tensor on a GPU")
+    device = gradients[0].device
+    outs = None if out is None else list(out)
+    if norm not in NORM:
+        _refuse(what, f"unknown norm {norm!r}")
+    if outs is not None and len(outs) != len(gradients):
+        _refuse(what, f"{len(outs)} outputs for {len(gradients)} gradients")
+    if stream is not None or device.index != _torch.cuda.current_device():
+        with _on(what, stream, device):
+            result = hbsjd_clip_gradients(gradients, max_norm, norm, outs)
+        if stream is not None:
+            for x in gradients + (outs or []):
+                x.record_stream(stream)
+        return result
+    types = []
+    for i, x in enumerate(gradients):
+        if not isinstance(x, _torch.Tensor) or x.device != device or x.dtype not in _types or not (x.is_contiguous() or _dense(x)):
+            _refuse(what, f"gradients[{i}] is not a dense tensor of fp32 or bf16 on {device}")
+        types.append(_types[x.dtype])
+    if outs is not None:
+        for i, (x, y) in enumerate(zip(gradients, outs)):
+            if not isinstance(y, _torch.Tensor) or y.device != device or y.dtype != x.dtype or y.shape != x.shape or (
+                    y.stride() != x.stride() and not (x.is_contiguous() and y.is_contiguous())):
+                _refuse(what, f"out[{i}] is not like gradients[{i}]")
+    n = len(gradients)
+    L = load()
+    result = _torch.empty((), dtype=_torch.float32, device=device)
+    work = _torch.empty((L.hbsjd_clip_workspace(n),), dtype=_torch.uint8, device=device)
+    _call(what, L.hbsjd_clip_gradients, device, hbsjd_clip_desc(n, NORM[norm], max_norm, 0),
+          (C.c_void_p * n)(*[x.data_ptr() for x in gradients]),
+          None if outs is None else (C.c_void_p * n)(*[x.data_ptr() for x in outs]),
+          (C.c_int64 * n)(*[x.numel() for x in gradients]), (C.c_int32 * n)(*types), work.data_ptr(), result.data_ptr())
+    if outs is not None or max_norm != float("inf"):
+        _torch.autograd.graph.increment_version(gradients if outs is None else outs)
+    return result
+
+
 class Context:
     """Owner of one hbsjd_ctx.  Methods carry the names of the C entry points."""
 
@@ -625,6 +856,23 @@ class Context:
                                               indices.data_ptr(), rest.data_ptr()), "hbsjd_score_topk")
         self.batch = 0
         return values, indices, rest
+
+    def hbsjd_score_logprobs(self, tokens, prefix_len, class_labels, temperature=1.0):
+        """Log-probabilities of the tokens of completed trajectories under this model, and the entropies of their distributions: (logp
+        fp32 [batch, T], entropy fp32 [batch, T]), device tensors; 0 for the prefixes."""
+        torch = self._torch
+        batch, T = tokens.shape[0], self.shape.T
+        assert tokens.is_cuda and tokens.dtype == torch.int32 and tokens.is_contiguous()
+        assert tuple(tokens.shape) == (batch, T)
+        for x in (prefix_len, class_labels):  # (read through their pointers, one per image)
+            assert x.is_cuda and x.device == tokens.device and x.dtype == torch.int32 and x.is_contiguous()
+            assert len(x.shape) == 1 and x.shape[0] >= batch
+        logp = torch.empty((batch, T), dtype=torch.float32, device=tokens.device)
+        entropy = torch.empty_like(logp)
+        self._check(self.lib.hbsjd_score_logprobs(self.h, batch, tokens.data_ptr(), prefix_len.data_ptr(), class_labels.data_ptr(),
+                                                  temperature, logp.data_ptr(), entropy.data_ptr()), "hbsjd_score_logprobs")
+        self.batch = 0
+        return logp, entropy
 
     def hbsjd_destroy(self):
         if self.h:

@@ -1300,6 +1300,56 @@ int score_topk(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32_t* pr
     return sync_counters(c);
 }
 
+// The forwards of one model, and the log-probabilities of the trajectories' own tokens.
+int score_logprobs(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32_t* prefix_len, const int32_t* class_labels, float temperature,
+                   float* logp, float* entropy) {
+    const int T = c->T, V = c->d.vocab;
+    if (!tokens || !prefix_len || !class_labels || !logp || batch < 1 || batch > c->Bmax || !is_temperature(temperature)) {
+        snprintf(c->err, sizeof(c->err), "hbsjd_score_logprobs: null argument, or batch %d or temperature %g out of range", batch, temperature);
+        return HBSJD_EINVAL;
+    }
+    if (const int rc = check_trajectories(c, batch, tokens, prefix_len, class_labels)) return rc;
+    const std::vector<int32_t> len(batch, T);  // every token of the sequences is an input
+    // (positions of the prefixes, which no row below has)
+    CK(cudaMemsetAsync(logp, 0, (size_t)batch * T * sizeof(float), c->stream));
+    if (entropy) CK(cudaMemsetAsync(entropy, 0, (size_t)batch * T * sizeof(float), c->stream));
+    score_begin(c, batch, tokens, prefix_len, class_labels, nullptr);
+    TokenArgs a = {};
+    a.x = c->activations;
+    a.ld = V;
+    a.V = V;
+    a.tokens = tokens;
+    a.logp = logp;
+    a.entropy = entropy;
+    a.temperature = temperature;
+    a.prefix_len = prefix_len;
+    a.T = T;
+    for (int done = 0, span; done < T; done += span) {
+        const PassShape sh = pass_shape(len, done, T, c->rows_cap);
+        span = sh.span;
+        if (const int rc = score_forward(c, sh)) return rc;
+        // logits and their tokens' in as few parts of equal size as there is room for
+        const int parts = (sh.rows + c->score_rows - 1) / c->score_rows;
+        const int step = std::min(c->score_rows, ((sh.rows + parts - 1) / parts + 127) / 128 * 128);
+        for (int row0 = 0; row0 < sh.rows; row0 += step) {
+            const int rows = std::min(step, sh.rows - row0);
+            float* out = (float*)c->activations;
+            const int rc = c->bf16_model ? head<bf16>(c, row0, rows, out, c->score_rows) : head<float>(c, row0, rows, out, c->score_rows);
+            if (rc) return rc;
+            a.at = c->st.row_pos + row0;
+            // timed with the vocabulary-wide class: V floats read per input
+            const int ps = prof_begin(c, HBSJD_PROF_ACCEPT, 4.0 * rows * V);
+            CK(launch_token(a, rows, HBSJD_DTYPE_FP32, c->stream));
+            prof_end(c, ps);
+            c->launches++;
+        }
+        launch_prefill_advance(c->st, span, c->stream);
+        c->launches++;
+    }
+    CK(cudaGetLastError());
+    return sync_counters(c);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1353,6 +1403,18 @@ int hbsjd_score_topk(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32
         return score_topk(c, batch, tokens, prefix_len, class_labels, k, temperature, values, indices, rest);
     } catch (const std::bad_alloc&) {
         snprintf(c->err, sizeof(c->err), "hbsjd_score_topk: out of host memory");
+        return HBSJD_ENOMEM;
+    }
+}
+
+int hbsjd_score_logprobs(hbsjd_ctx* c, int batch, const int32_t* tokens, const int32_t* prefix_len, const int32_t* class_labels,
+                         float temperature, float* logp, float* entropy) {
+    if (!c) return HBSJD_EINVAL;
+    c->err[0] = 0;
+    try {
+        return score_logprobs(c, batch, tokens, prefix_len, class_labels, temperature, logp, entropy);
+    } catch (const std::bad_alloc&) {
+        snprintf(c->err, sizeof(c->err), "hbsjd_score_logprobs: out of host memory");
         return HBSJD_ENOMEM;
     }
 }

@@ -515,6 +515,34 @@ cudaError_t launch_topk(const TopkArgs& a, int rows, int dtype, Stream& s);
 // empty lists for the positions of the images' prefixes (a.prefix_len, a.T)
 cudaError_t launch_topk_clear(const TopkArgs& a, int batch, Stream& s);
 
+struct TokenArgs {
+    const void* x;
+    int64_t ld, ld_g;
+    const int32_t* tokens;   // [rows]
+    const float* weight;     // [rows] or null; 0: the row is left out
+    const float *advantage, *old_logp, *ref;  // [rows]: the policy's loss; null: none, its own, no KL term
+    const float *d_logp, *d_entropy;          // [rows]: the gradient of these; null: the policy's, none
+    float *loss, *logp, *entropy;             // [rows] or null
+    void* grad;              // rows, or null
+    int rows, V, ctas, slice;
+    float temperature, low, high, dual, kl, bonus;
+    // rows of a scoring forward (see TopkArgs); tokens, logp and entropy are [batch][T] then
+    const int2* at;
+    const int32_t* prefix_len;
+    int T;
+};
+cudaError_t launch_token(const TokenArgs& a, int rows, int dtype, Stream& s);
+
+struct PairArgs {
+    const int32_t* offsets;  // [2 pairs + 1]
+    const float *logp, *ref, *weight, *pair_weight;  // [rows], [rows] or null, [rows] or null, [pairs] or null
+    float *loss, *sums;      // [pairs], [2 pairs]; null: not wanted
+    float* slope;            // [rows] or null
+    int rows, pairs, kind, interleaved;
+    float beta, smoothing, margin;
+};
+cudaError_t launch_pairs(const PairArgs& a, Stream& s);
+
 struct AdjustArgs {
     const void *x, *u;
     void* out;
