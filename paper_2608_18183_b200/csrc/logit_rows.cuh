@@ -524,6 +524,7 @@ struct TokenArgs {
     const float *d_logp, *d_entropy;          // [rows]: the gradient of these; null: the policy's, none
     float *loss, *logp, *entropy;             // [rows] or null
     void* grad;              // rows, or null
+    float4* stats;           // [rows] or null: m, z (see TokenSums), the mass of the others
     int rows, V, ctas, slice;
     float temperature, low, high, dual, kl, bonus;
     // rows of a scoring forward (see TopkArgs); tokens, logp and entropy are [batch][T] then
@@ -533,14 +534,28 @@ struct TokenArgs {
 };
 cudaError_t launch_token(const TokenArgs& a, int rows, int dtype, Stream& s);
 
+// The gradient of slope log q_token from a row's sums, the last rows first: those that were summed last may still be in L2.
+struct SpreadArgs {
+    const void* x;
+    void* grad;
+    int64_t ld, ld_g;
+    const int32_t* tokens;  // [rows]
+    const float* slope;     // [rows]; 0: the row is left out
+    const float4* stats;    // [rows]
+    int rows, V, parts, part;
+    float temperature;
+};
+cudaError_t launch_spread(const SpreadArgs& a, int rows, int dtype, Stream& s);
+
 struct PairArgs {
-    const int32_t* offsets;  // [2 pairs + 1]
+    const int32_t *offsets, *tokens;  // [2 pairs + 1], [rows]
     const float *logp, *ref, *weight, *pair_weight;  // [rows], [rows] or null, [rows] or null, [pairs] or null
     float *loss, *sums;      // [pairs], [2 pairs]; null: not wanted
     float* slope;            // [rows] or null
-    int rows, pairs, kind, interleaved;
+    int rows, V, pairs, kind, interleaved;
     float beta, smoothing, margin;
 };
+// directly behind launch_token, which makes logp
 cudaError_t launch_pairs(const PairArgs& a, Stream& s);
 
 struct AdjustArgs {

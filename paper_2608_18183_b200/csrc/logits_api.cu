@@ -319,7 +319,7 @@ int hbsjd_policy_loss(void* cuda_stream, const hbsjd_policy_desc* d, const void*
 }
 
 size_t hbsjd_preference_workspace(const hbsjd_preference_desc* d) {
-    return d && d->rows > 0 ? (size_t)d->rows * 8 : 0;  // log-probabilities and slopes of the rows
+    return d && d->rows > 0 ? (size_t)d->rows * 24 : 0;  // sums, log-probabilities and slopes of the rows
 }
 
 int hbsjd_preference_loss(void* cuda_stream, const hbsjd_preference_desc* d, const void* logits, const int32_t* tokens,
@@ -339,14 +339,18 @@ int hbsjd_preference_loss(void* cuda_stream, const hbsjd_preference_desc* d, con
     if (const int rc = words_wrong(what, offsets, ref_logp, weight, pair_weight, loss, sums, logp)) return rc;
     if (!is_aligned(workspace, 16)) return refuse("%s: the workspace is not aligned to 16 bytes", what);
     Stream s((cudaStream_t)cuda_stream);
-    float* slope = (float*)workspace + d->rows;
+    float4* stats = (float4*)workspace;
+    float *own = (float*)(stats + d->rows), *slope = own + d->rows;
     TokenArgs a = token_args(d, logits, tokens, nullptr);
     a.weight = weight;
-    a.logp = logp ? logp : (float*)workspace;
+    a.logp = logp ? logp : own;
+    a.stats = grad ? stats : nullptr;
     cudaError_t e = launch_token(a, d->rows, d->dtype, s);
     if (e != cudaSuccess) return launched(what, e);
     PairArgs p = {};
     p.offsets = offsets;
+    p.tokens = tokens;
+    p.V = d->V;
     p.logp = a.logp;
     p.ref = ref_logp;
     p.weight = weight;
@@ -363,9 +367,17 @@ int hbsjd_preference_loss(void* cuda_stream, const hbsjd_preference_desc* d, con
     p.margin = d->margin;
     e = launch_pairs(p, s);
     if (e != cudaSuccess || !grad) return launched(what, e);
-    a = token_args(d, logits, tokens, grad);
-    a.d_logp = slope;
-    return launched(what, launch_token(a, d->rows, d->dtype, s));
+    SpreadArgs g = {};
+    g.x = logits;
+    g.grad = grad;
+    g.ld = d->ld;
+    g.ld_g = d->ld_grad;
+    g.tokens = tokens;
+    g.slope = slope;
+    g.stats = stats;
+    g.V = d->V;
+    g.temperature = d->temperature;
+    return launched(what, launch_spread(g, d->rows, d->dtype, s));
 }
 
 size_t hbsjd_clip_workspace(int count) { return count > 0 ? sizeof(double) * CLIP_PARTS * clip_launches(count) : 0; }

@@ -12,19 +12,6 @@ namespace {
 
 constexpr int PAIR_THREADS = 256;
 
-__device__ __forceinline__ double sum_of_block(double v, double* parts) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if (lane == 0) parts[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.0;
-#pragma unroll
-    for (int i = 0; i < PAIR_THREADS / 32; ++i) v += parts[i];
-    return v;
-}
-
 // (loss, its slope in h)
 __device__ __forceinline__ double2 pair_loss(const PairArgs& a, double h) {
     if (a.kind == HBSJD_PREFERENCE_SQUARE) {
@@ -39,58 +26,64 @@ __device__ __forceinline__ double2 pair_loss(const PairArgs& a, double h) {
             a.beta * (e * up - (1.0 - e) * down)};
 }
 
-// A CTA a pair.
+// A CTA a pair, half of it a sequence.  What it reads of the caller's before it waits for the kernel in front was there before that one
+// began (see pdl_wait): the rows' log-probabilities are all that comes from it.
 __global__ void __launch_bounds__(PAIR_THREADS) k_pairs(PairArgs a) {
+    constexpr int HALF = PAIR_THREADS / 2;
     __shared__ double parts[PAIR_THREADS / 32];
-    pdl_wait();
-    pdl_trigger();
+    const int tid = threadIdx.x, pair = blockIdx.x, side = tid / HALF;
+    const int chosen = a.interleaved ? 2 * pair : pair, other = a.interleaved ? 2 * pair + 1 : a.pairs + pair, seq = side ? other : chosen;
     // offsets that decrease, or leave the rows: nothing is known of any sequence
     bool wrong = false;
-    for (int i = threadIdx.x; i <= 2 * a.pairs; i += PAIR_THREADS) {
+    for (int i = tid; i <= 2 * a.pairs; i += PAIR_THREADS) {
         const int at = __ldg(a.offsets + i), before = i ? __ldg(a.offsets + i - 1) : 0;
         wrong |= at < before || at > a.rows;
     }
+    // (whatever the offsets are, rows of the call's)
+    const int begin = min(max(__ldg(a.offsets + seq), 0), a.rows) + tid % HALF, end = min(__ldg(a.offsets + seq + 1), a.rows);
+    // a row's weight; 0: it is left out
+    const auto weight = [&](int r) {
+        const int t = __ldg(a.tokens + r);
+        return t < 0 || t >= a.V ? 0.f : a.weight ? __ldg(a.weight + r) : 1.f;
+    };
+    pdl_wait();
+    pdl_trigger();
+    double v = 0.0;
+#pragma unroll 4
+    for (int r = begin; r < end; r += HALF) {
+        const float w = weight(r), l = a.logp[r], ref = a.ref ? __ldg(a.ref + r) : 0.f;
+        if (w != 0.f) v += (double)w * ((double)l - (double)ref);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (tid % 32 == 0) parts[tid / 32] = v;
     wrong = __syncthreads_or(wrong);
-    const int pair = blockIdx.x;
-    const int seq[2] = {a.interleaved ? 2 * pair : pair, a.interleaved ? 2 * pair + 1 : a.pairs + pair};
+    double sum[2] = {0.0, 0.0};
+#pragma unroll
+    for (int i = 0; i < PAIR_THREADS / 32; ++i) sum[i / (HALF / 32)] += parts[i];
+    double2 f = pair_loss(a, sum[0] - sum[1]);
+    if (wrong) f.x = f.y = sum[0] = sum[1] = NAN;
+    if (tid == 0) {
+        if (a.loss) a.loss[pair] = (float)f.x;
+        if (a.sums) a.sums[chosen] = (float)sum[0], a.sums[other] = (float)sum[1];
+    }
+    if (!a.slope) return;
+    const int64_t all = (int64_t)PAIR_THREADS * gridDim.x, at = (int64_t)pair * PAIR_THREADS + tid;
     if (wrong) {
-        if (threadIdx.x == 0) {
-            if (a.loss) a.loss[pair] = NAN;
-            if (a.sums) a.sums[seq[0]] = a.sums[seq[1]] = NAN;
-        }
-        if (a.slope)
-            for (int64_t r = (int64_t)pair * PAIR_THREADS + threadIdx.x; r < a.rows; r += (int64_t)gridDim.x * PAIR_THREADS) a.slope[r] = NAN;
+        for (int64_t r = at; r < a.rows; r += all) a.slope[r] = NAN;
         return;
     }
-    double sum[2];
-    for (int k = 0; k < 2; ++k) {
-        const int end = __ldg(a.offsets + seq[k] + 1);
-        double v = 0.0;
-        for (int r = __ldg(a.offsets + seq[k]) + threadIdx.x; r < end; r += PAIR_THREADS) {
-            const float w = a.weight ? __ldg(a.weight + r) : 1.f;
-            if (w != 0.f) v += (double)w * ((double)a.logp[r] - (a.ref ? (double)__ldg(a.ref + r) : 0.0));
-        }
-        sum[k] = sum_of_block(v, parts);
+    const double slope = (side ? -f.y : f.y) * (a.pair_weight ? (double)__ldg(a.pair_weight + pair) : 1.0);
+#pragma unroll 4
+    for (int r = begin; r < end; r += HALF) {
+        const float w = weight(r);
+        a.slope[r] = w == 0.f ? 0.f : (float)(slope * w);
     }
-    const double2 f = pair_loss(a, sum[0] - sum[1]);
-    if (threadIdx.x == 0) {
-        if (a.loss) a.loss[pair] = (float)f.x;
-        if (a.sums) a.sums[seq[0]] = (float)sum[0], a.sums[seq[1]] = (float)sum[1];
-    }
-    if (a.slope) {
-        const double slope = f.y * (a.pair_weight ? (double)__ldg(a.pair_weight + pair) : 1.0);
-        for (int k = 0; k < 2; ++k) {
-            const int end = __ldg(a.offsets + seq[k] + 1);
-            for (int r = __ldg(a.offsets + seq[k]) + threadIdx.x; r < end; r += PAIR_THREADS) {
-                const float w = a.weight ? __ldg(a.weight + r) : 1.f;
-                a.slope[r] = w == 0.f ? 0.f : (float)(k ? -slope * w : slope * w);
-            }
-        }
-        // rows of no sequence
-        const int from = __ldg(a.offsets), to = __ldg(a.offsets + 2 * a.pairs);
-        for (int r = pair * PAIR_THREADS + threadIdx.x; r < a.rows; r += gridDim.x * PAIR_THREADS)
+    // rows of no sequence
+    const int from = __ldg(a.offsets), to = __ldg(a.offsets + 2 * a.pairs);
+    if (from > 0 || to < a.rows)
+        for (int64_t r = at; r < a.rows; r += all)
             if (r < from || r >= to) a.slope[r] = 0.f;
-    }
 }
 
 }  // namespace

@@ -1,67 +1,13 @@
 // Log-probabilities of sampled tokens, the clipped policy loss and what both give back to the logits, in one pass over memory.
-//
-// With x = logits / tau, q = softmax(x), t the row's token and o all others:
-//   D = log sum_o e^x - x_t,   l = log q_t = -log(1 + e^D),   sum_o q = 1 / (1 + e^-D),
-//   H = -sum q log q,          d (a l + b H) / dx_v = a (1[v = t] - q_v) - b q_v (log q_v + H).
-// The token leaves the row before the row is summed, so that neither l nor 1 - q_t is a difference of near numbers: a token of almost
-// all the mass has digits in both.  Two sums over the others (exponentials, and weighted by their exponents where the entropy is
-// wanted) give the loss, and a second look at the row the gradient.
+// (see token_rows.cuh for the formulas).  Two sums over a row (exponentials, and weighted by their exponents where the entropy is wanted)
+// give the loss, and a second look at the row the gradient.
 #include <type_traits>
 
-#include "logit_rows.cuh"
+#include "token_rows.cuh"
 
 namespace hbsjd {
 
 namespace {
-
-// Sums of e = 2^t, t = (x - m) c, over entries of a row, and of e t.
-struct TokenSums {
-    float m, z, a;
-    __device__ __forceinline__ static TokenSums none() { return {-INFINITY, 0.f, 0.f}; }
-};
-
-// No less than this is an exponent taken to be: 2^t is zero below 2^-126, and zero times it is zero.  NaN passes.
-__device__ __forceinline__ float held(float t) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(t), "f"(-200.f));
-    return r;
-}
-
-// G elements of a staged row; with FLOOR none below -1e30, so that exponents stay finite.  NaN passes.
-constexpr float FLOOR_VALUE = -1e30f;
-__device__ __forceinline__ float above(float x) {
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(FLOOR_VALUE));
-    return x;
-}
-template <bool FLOOR>
-__device__ __forceinline__ void read(const float* p, float (&x)[4]) {
-    get<4>(p, x);
-    if constexpr (FLOOR) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = above(x[i]);
-    }
-}
-template <bool FLOOR>
-__device__ __forceinline__ void read(const bf16* p, float (&x)[8]) {
-    uint4 v = *reinterpret_cast<const uint4*>(p);
-    uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (FLOOR) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(0xf149f149u));  // (-9.95e29)
-        unpack(w[i], x[2 * i], x[2 * i + 1]);
-    }
-}
-
-__device__ __forceinline__ void put2(float* p, float lo, float hi) { __stcs(reinterpret_cast<float2*>(p), make_float2(lo, hi)); }
-__device__ __forceinline__ void put2(bf16* p, float lo, float hi) { __stcs(reinterpret_cast<uint32_t*>(p), pack(lo, hi)); }
-
-// Where x c - m c may be taken as one multiply-add of x: t is as good as its own rounding, and m c is off by `rest`, less than 2^-4.
-__device__ __forceinline__ bool is_plain(float m, float c) { return fabsf(m) < 1e28f && fabsf(m * c) < 1048576.f && c > 1e-20f && c < 1e8f; }
-// 2^-rest
-__device__ __forceinline__ float less(float rest) {
-    const float y = rest * -LN2;
-    return fmaf(y, fmaf(y, fmaf(y, 1.f / 6, 0.5f), 1.f), 1.f);
-}
 
 template <bool ENT, int WARPS>
 __device__ __forceinline__ void post_sums(const TokenSums& x, TokenSums* slots, int ctas, int rank) {
@@ -91,23 +37,6 @@ __device__ __forceinline__ TokenSums collect_sums(const TokenSums* slots, int co
     return r;
 }
 
-// ln z of a normal z, within 2^-22 and its own rounding: the power of two apart, so that lg2 has its absolute error.
-__device__ __forceinline__ float ln(float z) {
-    const uint32_t b = __float_as_uint(z);
-    // (zero, infinities and NaN as lg2 has them)
-    const int k = b - 0x00800000u < 0x7f000000u ? (int)(b >> 23) - 127 : 0;
-    return LN2 * ((float)k + lg2(__uint_as_float(b - ((uint32_t)k << 23))));
-}
-
-// log(1 + s), s in 0..1, to its own last digits: 2 (u + u^3 / 3 + u^5 / 5 ...) with u = s / (2 + s), which leaves 1e-8 of it behind u^15.
-__device__ __forceinline__ float log1p_of(float s) {
-    const float u = __fdividef(s, 2.f + s), u2 = u * u;
-    float f = 1.f / 15;
-#pragma unroll
-    for (int i = 13; i > 0; i -= 2) f = fmaf(f, u2, 1.f / i);
-    return 2.f * u * f;
-}
-
 // e^d - 1 - d: by series where |d| < 3/4, whose next terms are below 7e-7 of it.
 __device__ __forceinline__ float exp_excess(float d) {
     if (fabsf(d) < 0.75f) {
@@ -118,18 +47,19 @@ __device__ __forceinline__ float exp_excess(float d) {
     return d > 40.f ? e : e - 1.f - d;
 }
 
-// What a row has besides its logits.
+// What a row has besides its logits: its weight, advantage, old and reference log-probability; or the slopes in log q and in the entropy.
 struct RowTerms {
-    float weight, A, old, ref, d_logp, d_entropy;
+    float a, b, c, d;
 };
 __device__ __forceinline__ RowTerms terms_of(const TokenArgs& a, int row) {
     const auto get = [&](const float* p, float other) { return p ? __ldg(p + row) : other; };
-    return {get(a.weight, 1.f), get(a.advantage, 0.f), get(a.old_logp, 0.f), get(a.ref, 0.f), get(a.d_logp, 0.f), get(a.d_entropy, 0.f)};
+    if (a.d_logp) return {__ldg(a.d_logp + row), get(a.d_entropy, 0.f), 0.f, 0.f};
+    return {get(a.weight, 1.f), get(a.advantage, 0.f), get(a.old_logp, 0.f), get(a.ref, 0.f)};
 }
 
 // The loss of a token whose log-probability is l, but for the entropy's part, and its slope in l.
 __device__ __forceinline__ float2 policy(const TokenArgs& a, const RowTerms& row, float l) {
-    const float A = row.A, r = !a.old_logp || l == row.old ? (l == l ? 1.f : l) : ex2((l - row.old) * LOG2E);
+    const float A = row.b, r = !a.old_logp || l == row.c ? (l == l ? 1.f : l) : ex2((l - row.c) * LOG2E);
     // (comparisons that let NaN pass; no advantage times an infinite ratio is none)
     const float low = 1.f - a.low, high = 1.f + a.high, clipped = r < low ? low : r > high ? high : r;
     const float kept = A == 0.f && r == INFINITY ? 0.f : r * A, other = clipped * A;
@@ -137,34 +67,12 @@ __device__ __forceinline__ float2 policy(const TokenArgs& a, const RowTerms& row
     if (a.dual > 0.f && A < 0.f && gain < a.dual * A) gain = a.dual * A, slope = 0.f;
     float loss = -gain;
     if (a.kl != 0.f && a.ref) {
-        const float d = l == row.ref ? 0.f : row.ref - l, excess = exp_excess(d);
+        const float d = l == row.d ? 0.f : row.d - l, excess = exp_excess(d);
         loss = fmaf(a.kl, excess, loss);
         slope = fmaf(-a.kl, d < -20.f ? -1.f : excess + d, slope);  // (e^d - 1)
     }
     return {loss, slope};
 }
-
-// each_group with a count of turns that all lanes share: where lanes differ in it, an unrolled loop runs its rest beside its last turn
-// (rows of 24001 bf16 took 15 turns' instructions for 12).
-template <int G, int WARPS, typename F>
-__device__ __forceinline__ void each_of(const Part<G, WARPS>& p, F&& f) {
-    const int lane = threadIdx.x & 31, inner = p.inner(), outer = p.outer();
-    int j = inner + lane;
-#pragma unroll 4
-    for (int left = (outer - inner) >> 5; left > 0; --left, j += 32) f(j, std::true_type());
-    if (j < outer) f(j, std::true_type());
-    // of the others, at most two hold some of the row: one in front, one behind
-    if (inner > p.j0 && lane == 0) f(inner - 1, std::false_type());
-    if (outer < p.j1 && lane == 1) f(outer, std::false_type());
-}
-
-// What a warp makes of a row's sums for its gradient.
-struct TokenCoefs {
-    int way;               // 0: k0, k1 as below; 1: the factors one by one; 2: no gradient
-    float mc, k0, k1;      // others: 2^t (k0 + k1 t), t = x c - mc
-    float token;           // the token's gradient
-    float m, K, A, B, base, scale;  // one by one: q = K 2^((x - m) c), scale q (B (ln2 t + base) - A)
-};
 
 template <typename T, bool ENT, bool GRAD, int THREADS, int PER_SM>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
@@ -172,7 +80,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     pdl_wait();
     pdl_trigger();
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int wid = threadIdx.x >> 5;
     const int rank = blockIdx.x % a.ctas, v0 = rank * a.slice, n = max(0, min(a.slice, a.V - v0));
     const int step = gridDim.x / a.ctas, places = WARPS * a.ctas;
     const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
@@ -211,25 +119,14 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
         const RowTerms terms = terms_of(a, row);
         T* g = GRAD ? (T*)a.grad + (int64_t)row * a.ld_g + v0 : nullptr;
         const T* x1 = x0 + stride;
-        const Part<G, WARPS> p1 = part_of(x1);
         bool fetched = t1 < 0;
         const int lo = p.first() - p.P, hi = p.last() - p.P;  // the warp's entries of the slice
         const bool first = rank == 0 && threadIdx.x == 0;
-        // Groups that are read for the last time make place for those of the next row: f(j, whole) of the warp's groups, and the copies.
         const auto each_then_next = [&](auto&& f) {
-            const int inner = p1.inner(), count = fetched ? 0 : p1.outer() - inner;
-            const T* base = x1 - p1.P;
-            each_of(p, [&](int j, auto whole) {
-                f(j, whole);
-                if ((unsigned)(j - inner) < (unsigned)count) cp_async16(ss + j * G, base + j * G);
-            });
-            if (!fetched) {
-                __syncwarp();
-                // (at another place behind 16 bytes a part may have groups that this one had not)
-                const int from = p.inner() - (p.inner() > p.j0), to = p.outer() + (p.outer() < p.j1);
-                for (int j = inner + lane; j < min(inner + count, from); j += 32) cp_async16(ss + j * G, base + j * G);
-                for (int j = max(inner, to) + lane; j < inner + count; j += 32) cp_async16(ss + j * G, base + j * G);
-                stage_ends(ss, x1, p1);
+            if (fetched) {
+                each_of(p, f);
+            } else {
+                each_then(ss, p, x1, part_of(x1), f);
                 fetched = true;
             }
         };
@@ -244,146 +141,187 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
             const int mine = t - v0 >= lo && t - v0 < hi ? t - v0 : -1;  // the token, if it is one of the warp's
             cp_async_wait_all();
             __syncwarp();
-            if (mine >= 0 && lane == 0) ss[p.P + mine] = from_f<T>(-INFINITY);
-            end_part(ss, p, -INFINITY);
-            // A warp sums against the largest logit of its first groups.  That overflows, or leaves nothing, in few rows; their warps
-            // find their maxima and look at every entry.
-            TokenSums v = TokenSums::none();
-            {
-                float x[G];
-                const int sample = p.inner() + lane;
-                if (sample < p.outer()) {
-                    get<G>(ss + sample * G, x);
-#pragma unroll
-                    for (int i = 0; i < G; ++i) v.m = fmaxf(v.m, x[i]);
-                }
-                v.m = max_of_warp(v.m);
-                __syncwarp();  // (the groups of the sample are other lanes' below, and may make place there)
-                const float mc = v.m * c;
-                const f32x2 o = both(-mc), c2 = both(c);
-                f32x2 z = both(0.f), w = z;
-                const auto add = [&](int j) {
-                    read<ENT>(ss + j * G, x);
-#pragma unroll
-                    for (int i = 0; i < G; i += 2) {
-                        const f32x2 e = fma2(both(x[i], x[i + 1]), c2, o), q = ex2(e);
-                        z = add2(z, q);
-                        if constexpr (ENT) w = fma2(q, e, w);
-                    }
-                };
-                // (one order of the sums, whatever is asked for)
-                if constexpr (!GRAD)
-                    each_then_next([&](int j, auto) { add(j); });
+            // (one order of the sums, whatever is asked for)
+            TokenSums v = part_sums<ENT>(ss, p, x0, mine, c, [&](auto&& f) {
+                if constexpr (GRAD)
+                    each_of(p, f);
                 else
-                    each_of(p, [&](int j, auto) { add(j); });
-                const float rest = fmaf(v.m, c, -mc), f = less(rest);
-                v.z = sum_of_warp(sum2(z)) * f;
-                if (ENT) v.a = fmaf(-rest, v.z, sum_of_warp(sum2(w)) * f);
-            }
-            if (!(v.z < 1e12f && v.z > 0.f && is_plain(v.m, c))) {
-                v = TokenSums::none();
-                for (int e = lo + lane; e < hi; e += 32)
-                    if (e != mine) v.m = fmaxf(v.m, to_f<T>(x0[e]));
-                v.m = max_of_warp(v.m);
-                const float o = v.m == -INFINITY ? 0.f : v.m;
-                for (int e = lo + lane; e < hi; e += 32)
-                    if (e != mine) {
-                        const float s = held((to_f<T>(x0[e]) - o) * c), q = ex2(s);
-                        v.z += q;
-                        v.a = fmaf(q, s, v.a);
-                    }
-                v.z = sum_of_warp(v.z);
-                v.a = sum_of_warp(v.a);
-            }
+                    each_then_next(f);
+            });
             post_sums<ENT, WARPS>(v, slots + parity * places, a.ctas, rank);
             posted(a.ctas);
             parity ^= 1;
             TokenCoefs k;
             if (GRAD || wid == 0) {  // (each warp for itself: one for all, and a barrier, cost 16384 rows of 16384 365 us in place of 351)
                 v = collect_sums<ENT>(slots + (parity ^ 1) * places, places, c);
-                const bool empty = v.z == 0.f && xt == -INFINITY;
-                // (an infinite logit: NaN)
-                const float lz = ln(v.z), D = xt < INFINITY ? fmaf(v.m - xt, inv_tau, lz) : NAN, s = ex2(-fabsf(D) * LOG2E);
-                // masses of the others and of the token
-                const float share = __fdividef(1.f, 1.f + s), qo = D > 0.f ? share : s * share, qt = D > 0.f ? s * share : share;
-                const float near = log1p_of(s), l = -(near + fmaxf(D, 0.f));
-                const float Lk = lz + (near + fmaxf(-D, 0.f));  // log q_v = ln2 t_v - Lk
+                const TokenRow r(v, xt, inv_tau);
                 float H = 0.f;
-                if (ENT) H = (v.z == 0.f || qo == 0.f ? 0.f : qo * (Lk - LN2 * __fdividef(v.a, v.z))) - (qt == 0.f ? 0.f : qt * l);
+                if (ENT && !r.empty) H = (v.z == 0.f || r.qo == 0.f ? 0.f : r.qo * (r.Lk - LN2 * __fdividef(v.a, v.z))) - (r.qt == 0.f ? 0.f : r.qt * r.l);
                 float2 f = {0.f, 0.f};
-                if (a.advantage) f = policy(a, terms, l);
+                if (a.advantage) f = policy(a, terms, r.l);
                 if (first) {
                     int64_t place = row;
                     if (a.at) {
                         const int2 at = __ldg(a.at + row);
                         place = (int64_t)at.x * a.T + at.y;
                     }
-                    if (a.loss) a.loss[row] = empty ? 0.f : a.bonus != 0.f ? fmaf(-a.bonus, H, f.x) : f.x;
-                    if (a.logp) a.logp[place] = empty ? -INFINITY : l == 0.f ? 0.f : l;
-                    if (ENT && a.entropy) a.entropy[place] = empty ? 0.f : H;
+                    if (a.loss) a.loss[row] = r.empty ? 0.f : a.bonus != 0.f ? fmaf(-a.bonus, H, f.x) : f.x;
+                    if (a.logp) a.logp[place] = r.logp();
+                    if (ENT && a.entropy) a.entropy[place] = H;
+                    if (!GRAD && a.stats) a.stats[row] = make_float4(v.m, v.z, r.empty ? 0.f : r.qo, 0.f);
                 }
-                if constexpr (GRAD) {
-                    k.scale = terms.weight * inv_tau, k.A = a.d_logp ? terms.d_logp : f.y, k.B = a.d_entropy ? -terms.d_entropy : a.bonus;
-                    k.m = v.m, k.mc = v.m * c, k.K = __fdividef(qo, v.z), k.base = H - Lk;
-                    const float rest = fmaf(v.m, c, -k.mc), f1 = less(rest);
-                    const float k0 = k.scale * k.K * (ENT ? fmaf(k.B, k.base, -k.A) : -k.A), k1 = ENT ? k.scale * k.K * k.B * LN2 : 0.f;
-                    k.k0 = fmaf(-k1, rest, k0) * f1, k.k1 = k1 * f1;
-                    float d = k.A * qo;
-                    if (ENT) d += k.B * (qt == 0.f ? 0.f : qt * (l + H));
-                    k.token = empty ? 0.f : k.scale * d;
-                    // (NaN passes)
-                    k.way = empty || (v.z == 0.f && xt < INFINITY) ? 2 : fabsf(k0) + fabsf(k1) < 1e30f && is_plain(v.m, c) ? 0 : 1;
-                }
+                if constexpr (GRAD)
+                    k.set<ENT>(r, v, H, a.d_logp ? terms.a : f.y, a.d_logp ? -terms.b : a.bonus, a.d_logp ? inv_tau : terms.a * inv_tau, c);
             }
-            if constexpr (GRAD) {
-                const int Pg = phase_of(g);  // the gradient is written wide, whatever the others' alignment
-                if (k.way == 2) {
-                    put_zeros(g, lo, hi);
-                } else if (k.way == 1) {
-                    for (int e = lo + lane; e < hi; e += 32) {
-                        const float u = held((to_f<T>(ss[p.P + e]) - k.m) * c), q = ex2(u) * k.K;
-                        const float m = ENT ? fmaf(k.B, fmaf(LN2, u, k.base), -k.A) : -k.A;
-                        g[e] = from_f<T>(q == 0.f ? 0.f : q * m * k.scale);
-                    }
-                } else {
-                    const f32x2 o = both(-k.mc), c2 = both(c), K0 = both(k.k0), K1 = both(k.k1);
-                    const auto of = [&](f32x2 x) {
-                        const f32x2 u = fma2(x, c2, o);
-                        return mul2(ex2(u), ENT ? fma2(K1, u, K0) : K0);
-                    };
-                    if (p.P == Pg) {
-                        T* out = g - p.P;
-                        each_then_next([&](int j, auto whole) {
-                            float x[G];
-                            read<ENT>(ss + j * G, x);
-#pragma unroll
-                            for (int i = 0; i < G; i += 2) split(of(both(x[i], x[i + 1])), x[i], x[i + 1]);
-                            if constexpr (decltype(whole)::value)
-                                put<G>(out + j * G, x);
-                            else
-                                put_at<T, G>(g, j * G - p.P, 0, n, x);
-                        });
-                    } else {  // two entries a lane: neighbours in the gradient, in order in shared memory
-                        for (int e = (lo + Pg) / 2 * 2 - Pg + lane * 2; e < hi; e += 64) {
-                            float x0 = to_f<T>(ss[p.P + max(e, lo)]), x1 = to_f<T>(ss[p.P + min(e + 1, hi - 1)]);
-                            if (ENT) x0 = above(x0), x1 = above(x1);
-                            split(of(both(x0, x1)), x0, x1);
-                            if (e >= lo && e + 1 < hi) {
-                                put2(g + e, x0, x1);
-                            } else {
-                                if (e >= lo) g[e] = from_f<T>(x0);
-                                if (e + 1 < hi) g[e + 1] = from_f<T>(x1);
-                            }
-                        }
-                    }
-                }
-                __syncwarp();  // the token's place was written above
-                if (mine >= 0 && lane == 0) g[mine] = from_f<T>(k.token);
-            }
+            if constexpr (GRAD) part_gradient<ENT>(ss, p, g, n, mine, k, c, each_then_next);
         }
         __syncwarp();  // the warp's part is done
+        x0 = x1, p = part_of(x0);
+        if (!fetched) stage_part(ss, x0, p);
+        t = t1, t1 = t2, xt = xt1;
+    }
+}
+
+// Whole rows are staged as in k_token, but nobody waits for anybody here.
+template <typename T, int THREADS, int PER_SM>
+__global__ void __launch_bounds__(THREADS, PER_SM) k_spread(SpreadArgs a) {
+    constexpr int G = 16 / sizeof(T), WARPS = THREADS / 32;
+    extern __shared__ __align__(16) unsigned char smem[];
+    pdl_wait();
+    pdl_trigger();
+    const int wid = threadIdx.x >> 5, step = gridDim.x;
+    const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
+    T* ss = (T*)smem;
+    struct Row {
+        float slope;
+        float4 stat;
+        int token;  // -1: the row is left out
+    };
+    const auto row_of = [&](int row) {
+        Row r = {0.f, {}, -1};
+        if (row < 0) return r;
+        r.slope = __ldg(a.slope + row), r.stat = __ldg(a.stats + row), r.token = __ldg(a.tokens + row);
+        if (r.slope == 0.f || r.token >= a.V) r.token = -1;
+        return r;
+    };
+    const auto part_of = [&](const T* x) { return Part<G, WARPS>(phase_of(x), a.V, wid); };
+    int row = a.rows - 1 - (int)blockIdx.x;
+    Row r = row_of(row), r1 = row_of(row - step);
+    const T* x0 = (const T*)a.x + (int64_t)row * a.ld;
+    Part<G, WARPS> p = part_of(x0);
+    if (r.token >= 0) stage_part(ss, x0, p);
+    for (; row >= 0; row -= step) {
+        const Row r2 = row_of(row - 2 * step);  // (so that no fetch waits for a slope)
+        const T* x1 = x0 - (int64_t)step * a.ld;
+        const Part<G, WARPS> p1 = part_of(x1);
+        T* g = (T*)a.grad + (int64_t)row * a.ld_g;
+        bool fetched = r1.token < 0;
+        const int lo = p.first() - p.P, hi = p.last() - p.P;  // the warp's entries
+        if (r.token < 0) {
+            put_zeros(g, lo, hi);
+        } else {
+            TokenSums v = TokenSums::none();
+            v.m = r.stat.x, v.z = r.stat.y;
+            TokenCoefs k;
+            k.set<false>(TokenRow(r.stat.y, r.stat.z), v, 0.f, r.slope, 0.f, inv_tau, c);
+            cp_async_wait_all();
+            __syncwarp();
+            part_gradient<false>(ss, p, g, a.V, r.token >= lo && r.token < hi ? r.token : -1, k, c, [&](auto&& f) {
+                if (fetched) {
+                    each_of(p, f);
+                } else {
+                    each_then(ss, p, x1, p1, f);
+                    fetched = true;
+                }
+            });
+        }
+        __syncwarp();
         if (!fetched) stage_part(ss, x1, p1);
-        t = t1, t1 = t2, xt = xt1, x0 = x1, p = p1;
+        r = r1, r1 = r2, x0 = x1, p = p1;
+    }
+}
+
+// No row waits for anything here: parts of rows of 8 KB, a warp each, from HBM to HBM.
+constexpr int SPREAD_THREADS = 256, SPREAD_WARPS = SPREAD_THREADS / 32, SPREAD_BYTES = 4096;
+template <typename T>
+__global__ void __launch_bounds__(SPREAD_THREADS, 4) k_spread_parts(SpreadArgs a) {
+    constexpr int G = 16 / sizeof(T), AHEAD = 4;  // groups a lane has on their way
+    pdl_wait();
+    pdl_trigger();
+    const int lane = threadIdx.x & 31;
+    const float inv_tau = 1.f / a.temperature, c = LOG2E * inv_tau;
+    const unsigned step = gridDim.x * SPREAD_WARPS, items = (unsigned)a.rows * a.parts;
+    unsigned u = blockIdx.x * SPREAD_WARPS + (threadIdx.x >> 5);
+    const auto row_of = [&](unsigned u) { return a.rows - 1 - (int)(u / a.parts); };
+    float slope = u < items ? __ldg(a.slope + row_of(u)) : 0.f;
+    float4 stat = u < items ? __ldg(a.stats + row_of(u)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    int token = u < items ? __ldg(a.tokens + row_of(u)) : -1;
+    for (; u < items; u += step) {
+        const int row = row_of(u), v0 = (int)(u % a.parts) * a.part, n = min(a.part, a.V - v0);
+        const T* x = (const T*)a.x + (int64_t)row * a.ld + v0;
+        T* g = (T*)a.grad + (int64_t)row * a.ld_g + v0;
+        const unsigned u1 = u + step;
+        float slope1 = 0.f;
+        float4 stat1 = {};
+        int token1 = -1;
+        if (u1 < items) slope1 = __ldg(a.slope + row_of(u1)), stat1 = __ldg(a.stats + row_of(u1)), token1 = __ldg(a.tokens + row_of(u1));
+        if (slope == 0.f || token < 0 || token >= a.V) {
+            put_zeros(g, 0, n);
+        } else {
+            TokenSums v = TokenSums::none();
+            v.m = stat.x, v.z = stat.y;
+            TokenCoefs k;
+            k.set<false>(TokenRow(stat.y, stat.z), v, 0.f, slope, 0.f, inv_tau, c);
+            const f32x2 o = both(-k.mc), c2 = both(c), K0 = both(k.k0);
+            const auto of = [&](f32x2 e) { return mul2(ex2(fma2(e, c2, o)), K0); };
+            const int P = phase_of(x), first = P ? G - P : 0, groups = max(0, n - first) / G;  // whole groups of 16 bytes from x + first
+            if (k.way == 2) {
+                put_zeros(g, 0, n);
+            } else if (k.way == 1 || P != phase_of(g)) {
+                for (int e = lane; e < n; e += 32) {
+                    const float y = to_f<T>(x[e]);
+                    float lo, hi;
+                    if (k.way == 1) {
+                        const float q = ex2(held((y - k.m) * c)) * k.K;
+                        lo = q == 0.f ? 0.f : q * -k.A * k.scale;
+                    } else {
+                        split(of(both(y, y)), lo, hi);
+                    }
+                    g[e] = from_f<T>(lo);
+                }
+            } else {
+                const T* xs = x + first;
+                T* gs = g + first;
+                for (int j0 = 0; j0 < groups; j0 += 32 * AHEAD) {
+                    uint4 w[AHEAD];
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i) {
+                        const int j = j0 + i * 32 + lane;
+                        if (j < groups) w[i] = __ldcs(reinterpret_cast<const uint4*>(xs) + j);
+                    }
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i) {
+                        const int j = j0 + i * 32 + lane;
+                        float y[G];
+                        read<false>(reinterpret_cast<const T*>(&w[i]), y);
+#pragma unroll
+                        for (int e = 0; e < G; e += 2) split(of(both(y[e], y[e + 1])), y[e], y[e + 1]);
+                        if (j < groups) put<G>(gs + j * G, y);
+                    }
+                }
+                // what is left in front and behind, less than 16 bytes each
+                const int tail = first + groups * G;
+                const int e = lane < 16 ? lane : tail + lane - 16;
+                if (lane < 16 ? lane < min(first, n) : e < n) {
+                    float lo, hi;
+                    split(of(both(to_f<T>(x[e]))), lo, hi);
+                    g[e] = from_f<T>(lo);
+                }
+            }
+            __syncwarp();  // the token's place was written above
+            if (token >= v0 && token - v0 < n && lane == 0) g[token - v0] = from_f<T>(k.token);
+        }
+        slope = slope1, stat = stat1, token = token1;
     }
 }
 
@@ -435,6 +373,36 @@ cudaError_t run_token(const TokenArgs& a, bool entropy, Stream& s) {
     return entropy ? run_token<T, true, false>(a, s) : run_token<T, false, false>(a, s);
 }
 
+template <typename T>
+cudaError_t run_spread(const SpreadArgs& args, Stream& s) {
+    SpreadArgs a = args;
+    const int sms = device_sm_count();
+    if constexpr (sizeof(T) == 4) {
+        // Rows of 64 fp32 KB on 256 threads, two an SM, or smaller ones alike; staged whole for the same order of reads and writes in HBM as
+        // theirs in k_token (16 pairs of 256 positions of 16384 266 us, of 16385 300; by parts 269 and 333).  In bf16, parts are as fast
+        // (64 pairs of 64 of 16384 148 and 153 us, 20 of 256 of 24001 306 and 277).
+        const size_t smem = (a.V + 24) / 8 * 8 * sizeof(T);
+        const int fit = (int)(227 * 1024 / (smem + 1024 + 128));  // (1 KB is the system's)
+        const auto run = [&](auto threads) {
+            constexpr int THREADS = decltype(threads)::value, PER_SM = 512 / THREADS;
+            const cudaError_t e = allow_row_smem<k_spread<T, THREADS, PER_SM>>();
+            if (e != cudaSuccess) return e;
+            return launch_kc(true, k_spread<T, THREADS, PER_SM>, dim3((unsigned)std::min(a.rows, sms * std::min(PER_SM, fit))), dim3(THREADS), smem, s, 1, a);
+        };
+        if (a.rows > sms && smem <= SHARED_SM) {
+            if (fit <= 3) return run(std::integral_constant<int, 256>());
+            if (fit <= 6) return run(std::integral_constant<int, 128>());
+            if (fit <= 14) return run(std::integral_constant<int, 64>());
+        }
+    }
+    const int most = SPREAD_BYTES / (int)sizeof(T);
+    a.parts = (a.V + most - 1) / most;
+    a.part = ((a.V + a.parts - 1) / a.parts + 7) / 8 * 8;
+    const int64_t items = (int64_t)a.rows * a.parts;
+    const dim3 grid((unsigned)std::min<int64_t>((int64_t)sms * 4, (items + SPREAD_WARPS - 1) / SPREAD_WARPS));
+    return launch_k(k_spread_parts<T>, grid, dim3(SPREAD_THREADS), 0, s, a);
+}
+
 }  // namespace
 
 cudaError_t launch_token(const TokenArgs& args, int rows, int dtype, Stream& s) {
@@ -443,6 +411,12 @@ cudaError_t launch_token(const TokenArgs& args, int rows, int dtype, Stream& s) 
     a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice;
     const bool entropy = a.entropy || a.d_entropy || a.bonus != 0.f;
     return dtype ? run_token<bf16>(a, entropy, s) : run_token<float>(a, entropy, s);
+}
+
+cudaError_t launch_spread(const SpreadArgs& args, int rows, int dtype, Stream& s) {
+    SpreadArgs a = args;
+    a.rows = rows;
+    return dtype ? run_spread<bf16>(a, s) : run_spread<float>(a, s);
 }
 
 }  // namespace hbsjd

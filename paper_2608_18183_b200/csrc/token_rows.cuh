@@ -1,0 +1,256 @@
+// What the operators on rows and their tokens have in common: a warp's sums over its part of a staged row without the row's token, what
+// the sums say of the token, and the part's gradient.
+//
+// With x = logits / tau, q = softmax(x), t the row's token and o all others:
+//   D = log sum_o e^x - x_t,   l = log q_t = -log(1 + e^D),   sum_o q = 1 / (1 + e^-D),
+//   H = -sum q log q,          d (a l + b H) / dx_v = a (1[v = t] - q_v) - b q_v (log q_v + H).
+// The token leaves the row before the row is summed, so that neither l nor 1 - q_t is a difference of near numbers: a token of almost
+// all the mass has digits in both.
+#pragma once
+#include "logit_rows.cuh"
+
+namespace hbsjd {
+
+// Sums of e = 2^t, t = (x - m) c, over entries of a row, and of e t.
+struct TokenSums {
+    float m, z, a;
+    __device__ __forceinline__ static TokenSums none() { return {-INFINITY, 0.f, 0.f}; }
+};
+
+// No less than this is an exponent taken to be: 2^t is zero below 2^-126, and zero times it is zero.  NaN passes.
+__device__ __forceinline__ float held(float t) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(t), "f"(-200.f));
+    return r;
+}
+
+// G elements of a staged row; with FLOOR none below -1e30, so that exponents stay finite.  NaN passes.
+constexpr float FLOOR_VALUE = -1e30f;
+__device__ __forceinline__ float above(float x) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x) : "f"(FLOOR_VALUE));
+    return x;
+}
+template <bool FLOOR>
+__device__ __forceinline__ void read(const float* p, float (&x)[4]) {
+    get<4>(p, x);
+    if constexpr (FLOOR) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = above(x[i]);
+    }
+}
+template <bool FLOOR>
+__device__ __forceinline__ void read(const bf16* p, float (&x)[8]) {
+    uint4 v = *reinterpret_cast<const uint4*>(p);
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (FLOOR) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(0xf149f149u));  // (-9.95e29)
+        unpack(w[i], x[2 * i], x[2 * i + 1]);
+    }
+}
+
+__device__ __forceinline__ void put2(float* p, float lo, float hi) { __stcs(reinterpret_cast<float2*>(p), make_float2(lo, hi)); }
+__device__ __forceinline__ void put2(bf16* p, float lo, float hi) { __stcs(reinterpret_cast<uint32_t*>(p), pack(lo, hi)); }
+
+// Where x c - m c may be taken as one multiply-add of x: t is as good as its own rounding, and m c is off by `rest`, less than 2^-4.
+__device__ __forceinline__ bool is_plain(float m, float c) { return fabsf(m) < 1e28f && fabsf(m * c) < 1048576.f && c > 1e-20f && c < 1e8f; }
+// 2^-rest
+__device__ __forceinline__ float less(float rest) {
+    const float y = rest * -LN2;
+    return fmaf(y, fmaf(y, fmaf(y, 1.f / 6, 0.5f), 1.f), 1.f);
+}
+
+// ln z of a normal z, within 2^-22 and its own rounding: the power of two apart, so that lg2 has its absolute error.
+__device__ __forceinline__ float ln(float z) {
+    const uint32_t b = __float_as_uint(z);
+    // (zero, infinities and NaN as lg2 has them)
+    const int k = b - 0x00800000u < 0x7f000000u ? (int)(b >> 23) - 127 : 0;
+    return LN2 * ((float)k + lg2(__uint_as_float(b - ((uint32_t)k << 23))));
+}
+
+// log(1 + s), s in 0..1, to its own last digits: 2 (u + u^3 / 3 + u^5 / 5 ...) with u = s / (2 + s), which leaves 1e-8 of it behind u^15.
+__device__ __forceinline__ float log1p_of(float s) {
+    const float u = __fdividef(s, 2.f + s), u2 = u * u;
+    float f = 1.f / 15;
+#pragma unroll
+    for (int i = 13; i > 0; i -= 2) f = fmaf(f, u2, 1.f / i);
+    return 2.f * u * f;
+}
+
+// each_group with a count of turns that all lanes share: where lanes differ in it, an unrolled loop runs its rest beside its last turn
+// (rows of 24001 bf16 took 15 turns' instructions for 12).
+template <int G, int WARPS, typename F>
+__device__ __forceinline__ void each_of(const Part<G, WARPS>& p, F&& f) {
+    const int lane = threadIdx.x & 31, inner = p.inner(), outer = p.outer();
+    int j = inner + lane;
+#pragma unroll 4
+    for (int left = (outer - inner) >> 5; left > 0; --left, j += 32) f(j, std::true_type());
+    if (j < outer) f(j, std::true_type());
+    // of the others, at most two hold some of the row: one in front, one behind
+    if (inner > p.j0 && lane == 0) f(inner - 1, std::false_type());
+    if (outer < p.j1 && lane == 1) f(outer, std::false_type());
+}
+
+// A warp's sums over its part of a slice at x0, staged at ss; `mine`: the token's place in the slice, if it is one of the part's, else -1.
+// walk(f) has f read every group of the part in one order.  A warp sums against the largest logit of its first groups.  That
+// overflows, or leaves nothing, in few rows; their warps find their maxima and look at every entry.
+template <bool ENT, typename T, int G, int WARPS, typename W>
+__device__ __forceinline__ TokenSums part_sums(T* ss, const Part<G, WARPS>& p, const T* x0, int mine, float c, W&& walk) {
+    const int lane = threadIdx.x & 31, lo = p.first() - p.P, hi = p.last() - p.P;
+    if (mine >= 0 && lane == 0) ss[p.P + mine] = from_f<T>(-INFINITY);
+    end_part(ss, p, -INFINITY);
+    TokenSums v = TokenSums::none();
+    float x[G];
+    const int sample = p.inner() + lane;
+    if (sample < p.outer()) {
+        get<G>(ss + sample * G, x);
+#pragma unroll
+        for (int i = 0; i < G; ++i) v.m = fmaxf(v.m, x[i]);
+    }
+    v.m = max_of_warp(v.m);
+    __syncwarp();  // (the groups of the sample are other lanes' below, and may make place there)
+    const float mc = v.m * c;
+    const f32x2 o = both(-mc), c2 = both(c);
+    f32x2 z = both(0.f), w = z;
+    walk([&](int j, auto) {
+        read<ENT>(ss + j * G, x);
+#pragma unroll
+        for (int i = 0; i < G; i += 2) {
+            const f32x2 e = fma2(both(x[i], x[i + 1]), c2, o), q = ex2(e);
+            z = add2(z, q);
+            if constexpr (ENT) w = fma2(q, e, w);
+        }
+    });
+    const float rest = fmaf(v.m, c, -mc), f = less(rest);
+    v.z = sum_of_warp(sum2(z)) * f;
+    if (ENT) v.a = fmaf(-rest, v.z, sum_of_warp(sum2(w)) * f);
+    if (!(v.z < 1e12f && v.z > 0.f && is_plain(v.m, c))) {
+        v = TokenSums::none();
+        for (int e = lo + lane; e < hi; e += 32)
+            if (e != mine) v.m = fmaxf(v.m, to_f<T>(x0[e]));
+        v.m = max_of_warp(v.m);
+        const float base = v.m == -INFINITY ? 0.f : v.m;
+        for (int e = lo + lane; e < hi; e += 32)
+            if (e != mine) {
+                const float s = held((to_f<T>(x0[e]) - base) * c), q = ex2(s);
+                v.z += q;
+                v.a = fmaf(q, s, v.a);
+            }
+        v.z = sum_of_warp(v.z);
+        v.a = sum_of_warp(v.a);
+    }
+    return v;
+}
+
+// What a row's sums over the others and its token's logit say.
+struct TokenRow {
+    bool empty;      // nothing has mass
+    bool alone;      // the token alone has
+    float l, qo, qt; // log q of the token, masses of the others and of the token
+    float Lk;        // log q_v = ln2 t_v - Lk
+    // of what was kept of one
+    __device__ __forceinline__ TokenRow(float z, float others) : empty(false), alone(z == 0.f && others == 0.f), l(0.f), qo(others), qt(0.f), Lk(0.f) {}
+    __device__ __forceinline__ TokenRow() {}
+    __device__ __forceinline__ TokenRow(const TokenSums& v, float xt, float inv_tau) {
+        empty = v.z == 0.f && xt == -INFINITY;
+        alone = v.z == 0.f && xt < INFINITY;
+        // (an infinite logit: NaN)
+        const float lz = ln(v.z), D = xt < INFINITY ? fmaf(v.m - xt, inv_tau, lz) : NAN, s = ex2(-fabsf(D) * LOG2E);
+        const float share = __fdividef(1.f, 1.f + s);
+        qo = D > 0.f ? share : s * share, qt = D > 0.f ? s * share : share;
+        const float near = log1p_of(s);
+        l = -(near + fmaxf(D, 0.f));
+        Lk = lz + (near + fmaxf(-D, 0.f));
+    }
+    __device__ __forceinline__ float logp() const { return empty ? -INFINITY : l == 0.f ? 0.f : l; }
+};
+
+// What a warp makes of a row's sums for its gradient.
+struct TokenCoefs {
+    int way;               // 0: k0, k1 as below; 1: the factors one by one; 2: no gradient
+    float mc, k0, k1;      // others: 2^t (k0 + k1 t), t = x c - mc
+    float token;           // the token's gradient
+    float m, K, A, B, base, scale;  // one by one: q = K 2^((x - m) c), scale q (B (ln2 t + base) - A)
+    // a (1[v = t] - q_v) + b q_v (log q_v + H), times scale
+    template <bool ENT>
+    __device__ __forceinline__ void set(const TokenRow& r, const TokenSums& v, float H, float a, float b, float s, float c) {
+        A = a, B = b, scale = s, m = v.m, mc = v.m * c, K = __fdividef(r.qo, v.z), base = ENT ? H - r.Lk : 0.f;
+        const float rest = fmaf(v.m, c, -mc), f = less(rest);
+        const float y0 = scale * K * (ENT ? fmaf(B, base, -A) : -A), y1 = ENT ? scale * K * B * LN2 : 0.f;
+        k0 = fmaf(-y1, rest, y0) * f, k1 = y1 * f;
+        float d = A * r.qo;
+        if (ENT) d += B * (r.qt == 0.f ? 0.f : r.qt * (r.l + H));
+        token = r.empty ? 0.f : scale * d;
+        // (NaN passes)
+        way = r.empty || r.alone ? 2 : fabsf(y0) + fabsf(y1) < 1e30f && is_plain(v.m, c) ? 0 : 1;
+    }
+};
+
+
+// A warp's part of the gradient at g, n entries of which are the slice's.  walk(f): as above.
+template <bool ENT, typename T, int G, int WARPS, typename W>
+__device__ __forceinline__ void part_gradient(const T* ss, const Part<G, WARPS>& p, T* g, int n, int mine, const TokenCoefs& k, float c, W&& walk) {
+    const int lane = threadIdx.x & 31, lo = p.first() - p.P, hi = p.last() - p.P, Pg = phase_of(g);
+    if (k.way == 2) {
+        put_zeros(g, lo, hi);
+    } else if (k.way == 1) {
+        for (int e = lo + lane; e < hi; e += 32) {
+            const float u = held((to_f<T>(ss[p.P + e]) - k.m) * c), q = ex2(u) * k.K;
+            const float m = ENT ? fmaf(k.B, fmaf(LN2, u, k.base), -k.A) : -k.A;
+            g[e] = from_f<T>(q == 0.f ? 0.f : q * m * k.scale);
+        }
+    } else {
+        const f32x2 o = both(-k.mc), c2 = both(c), K0 = both(k.k0), K1 = both(k.k1);
+        const auto of = [&](f32x2 x) {
+            const f32x2 u = fma2(x, c2, o);
+            return mul2(ex2(u), ENT ? fma2(K1, u, K0) : K0);
+        };
+        if (p.P == Pg) {
+            T* out = g - p.P;
+            walk([&](int j, auto whole) {
+                float x[G];
+                read<ENT>(ss + j * G, x);
+#pragma unroll
+                for (int i = 0; i < G; i += 2) split(of(both(x[i], x[i + 1])), x[i], x[i + 1]);
+                if constexpr (decltype(whole)::value)
+                    put<G>(out + j * G, x);
+                else
+                    put_at<T, G>(g, j * G - p.P, 0, n, x);
+            });
+        } else {  // two entries a lane: neighbours in the gradient, in order in shared memory
+            for (int e = (lo + Pg) / 2 * 2 - Pg + lane * 2; e < hi; e += 64) {
+                float x0 = to_f<T>(ss[p.P + max(e, lo)]), x1 = to_f<T>(ss[p.P + min(e + 1, hi - 1)]);
+                if (ENT) x0 = above(x0), x1 = above(x1);
+                split(of(both(x0, x1)), x0, x1);
+                if (e >= lo && e + 1 < hi) {
+                    put2(g + e, x0, x1);
+                } else {
+                    if (e >= lo) g[e] = from_f<T>(x0);
+                    if (e + 1 < hi) g[e + 1] = from_f<T>(x1);
+                }
+            }
+        }
+    }
+    __syncwarp();  // the token's place was written above
+    if (mine >= 0 && lane == 0) g[mine] = from_f<T>(k.token);
+}
+
+// Reads every group of a part p for the last time, f(j, whole), and has each make place for the same group of the part p1 of a slice at
+// x1, whose copies have begun when it returns.
+template <typename T, int G, int WARPS, typename F>
+__device__ __forceinline__ void each_then(T* ss, const Part<G, WARPS>& p, const T* x1, const Part<G, WARPS>& p1, F&& f) {
+    const int lane = threadIdx.x & 31, inner = p1.inner(), count = p1.outer() - inner;
+    const T* base = x1 - p1.P;
+    each_of(p, [&](int j, auto whole) {
+        f(j, whole);
+        if ((unsigned)(j - inner) < (unsigned)count) cp_async16(ss + j * G, base + j * G);
+    });
+    __syncwarp();
+    // (at another place behind 16 bytes, or of another length, a part may have groups that this one had not)
+    const int from = p.inner() - (p.inner() > p.j0), to = p.outer() + (p.outer() < p.j1);
+    for (int j = inner + lane; j < min(inner + count, from); j += 32) cp_async16(ss + j * G, base + j * G);
+    for (int j = max(inner, to) + lane; j < inner + count; j += 32) cp_async16(ss + j * G, base + j * G);
+    stage_ends(ss, x1, p1);
+}
+
+}  // namespace hbsjd
