@@ -119,16 +119,13 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
         const RowTerms terms = terms_of(a, row);
         T* g = GRAD ? (T*)a.grad + (int64_t)row * a.ld_g + v0 : nullptr;
         const T* x1 = x0 + stride;
+        const Part<G, WARPS> p1 = part_of(x1);
         bool fetched = t1 < 0;
         const int lo = p.first() - p.P, hi = p.last() - p.P;  // the warp's entries of the slice
         const bool first = rank == 0 && threadIdx.x == 0;
         const auto each_then_next = [&](auto&& f) {
-            if (fetched) {
-                each_of(p, f);
-            } else {
-                each_then(ss, p, x1, part_of(x1), f);
-                fetched = true;
-            }
+            each_then(ss, p, !fetched, x1, p1, f);
+            fetched = true;
         };
         if (t < 0) {  // (all CTAs of the row)
             if constexpr (GRAD) put_zeros(g, lo, hi);
@@ -148,12 +145,15 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
                 else
                     each_then_next(f);
             });
-            post_sums<ENT, WARPS>(v, slots + parity * places, a.ctas, rank);
-            posted(a.ctas);
-            parity ^= 1;
+            const bool alone = WARPS == 1 && a.ctas == 1;  // the warp has the whole row
+            if (!alone) {
+                post_sums<ENT, WARPS>(v, slots + parity * places, a.ctas, rank);
+                posted(a.ctas);
+                parity ^= 1;
+            }
             TokenCoefs k;
             if (GRAD || wid == 0) {  // (each warp for itself: one for all, and a barrier, cost 16384 rows of 16384 365 us in place of 351)
-                v = collect_sums<ENT>(slots + (parity ^ 1) * places, places, c);
+                if (!alone) v = collect_sums<ENT>(slots + (parity ^ 1) * places, places, c);
                 const TokenRow r(v, xt, inv_tau);
                 float H = 0.f;
                 if (ENT && !r.empty) H = (v.z == 0.f || r.qo == 0.f ? 0.f : r.qo * (r.Lk - LN2 * __fdividef(v.a, v.z))) - (r.qt == 0.f ? 0.f : r.qt * r.l);
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
             if constexpr (GRAD) part_gradient<ENT>(ss, p, g, n, mine, k, c, each_then_next);
         }
         __syncwarp();  // the warp's part is done
-        x0 = x1, p = part_of(x0);
+        x0 = x1, p = p1;
         if (!fetched) stage_part(ss, x0, p);
         t = t1, t1 = t2, xt = xt1;
     }
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_spread(SpreadArgs a) {
                 if (fetched) {
                     each_of(p, f);
                 } else {
-                    each_then(ss, p, x1, p1, f);
+                    each_then(ss, p, true, x1, p1, f);
                     fetched = true;
                 }
             });

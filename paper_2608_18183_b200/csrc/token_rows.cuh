@@ -235,22 +235,25 @@ __device__ __forceinline__ void part_gradient(const T* ss, const Part<G, WARPS>&
     if (mine >= 0 && lane == 0) g[mine] = from_f<T>(k.token);
 }
 
-// Reads every group of a part p for the last time, f(j, whole), and has each make place for the same group of the part p1 of a slice at
-// x1, whose copies have begun when it returns.
+// Reads every group of a part p for the last time, f(j, whole), and, if there is one to come, has each make place for the same group of the
+// part p1 of a slice at x1, whose copies have begun when it returns.  (One loop for both: two of them in a kernel cost 8192 bf16 rows of
+// 16384 with entropy and gradient 115 us in place of 109.)
 template <typename T, int G, int WARPS, typename F>
-__device__ __forceinline__ void each_then(T* ss, const Part<G, WARPS>& p, const T* x1, const Part<G, WARPS>& p1, F&& f) {
-    const int lane = threadIdx.x & 31, inner = p1.inner(), count = p1.outer() - inner;
+__device__ __forceinline__ void each_then(T* ss, const Part<G, WARPS>& p, bool more, const T* x1, const Part<G, WARPS>& p1, F&& f) {
+    const int lane = threadIdx.x & 31, inner = p1.inner(), count = more ? p1.outer() - inner : 0;
     const T* base = x1 - p1.P;
     each_of(p, [&](int j, auto whole) {
         f(j, whole);
         if ((unsigned)(j - inner) < (unsigned)count) cp_async16(ss + j * G, base + j * G);
     });
-    __syncwarp();
-    // (at another place behind 16 bytes, or of another length, a part may have groups that this one had not)
-    const int from = p.inner() - (p.inner() > p.j0), to = p.outer() + (p.outer() < p.j1);
-    for (int j = inner + lane; j < min(inner + count, from); j += 32) cp_async16(ss + j * G, base + j * G);
-    for (int j = max(inner, to) + lane; j < inner + count; j += 32) cp_async16(ss + j * G, base + j * G);
-    stage_ends(ss, x1, p1);
+    if (more) {
+        __syncwarp();
+        // (at another place behind 16 bytes a part may have groups that this one had not)
+        const int from = p.inner() - (p.inner() > p.j0), to = p.outer() + (p.outer() < p.j1);
+        for (int j = inner + lane; j < min(inner + count, from); j += 32) cp_async16(ss + j * G, base + j * G);
+        for (int j = max(inner, to) + lane; j < inner + count; j += 32) cp_async16(ss + j * G, base + j * G);
+        stage_ends(ss, x1, p1);
+    }
 }
 
 }  // namespace hbsjd
