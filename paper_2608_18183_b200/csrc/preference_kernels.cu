@@ -26,21 +26,19 @@ __device__ __forceinline__ double2 pair_loss(const PairArgs& a, double h) {
             a.beta * (e * up - (1.0 - e) * down)};
 }
 
-// A CTA a pair, half of it a sequence.  What it reads of the caller's before it waits for the kernel in front was there before that one
+// A CTA a pair (or several in turn: each looks at all offsets), half of it a sequence.  What it reads of the caller's before it waits for the kernel in front was there before that one
 // began (see pdl_wait): the rows' log-probabilities are all that comes from it.
 __global__ void __launch_bounds__(PAIR_THREADS) k_pairs(PairArgs a) {
     constexpr int HALF = PAIR_THREADS / 2;
     __shared__ double parts[PAIR_THREADS / 32];
-    const int tid = threadIdx.x, pair = blockIdx.x, side = tid / HALF;
-    const int chosen = a.interleaved ? 2 * pair : pair, other = a.interleaved ? 2 * pair + 1 : a.pairs + pair, seq = side ? other : chosen;
+    const int tid = threadIdx.x, side = tid / HALF;
     // offsets that decrease, or leave the rows: nothing is known of any sequence
     bool wrong = false;
     for (int i = tid; i <= 2 * a.pairs; i += PAIR_THREADS) {
         const int at = __ldg(a.offsets + i), before = i ? __ldg(a.offsets + i - 1) : 0;
         wrong |= at < before || at > a.rows;
     }
-    // (whatever the offsets are, rows of the call's)
-    const int begin = min(max(__ldg(a.offsets + seq), 0), a.rows) + tid % HALF, end = min(__ldg(a.offsets + seq + 1), a.rows);
+    const int from = __ldg(a.offsets), to = __ldg(a.offsets + 2 * a.pairs);
     // a row's weight; 0: it is left out
     const auto weight = [&](int r) {
         const int t = __ldg(a.tokens + r);
@@ -48,48 +46,53 @@ __global__ void __launch_bounds__(PAIR_THREADS) k_pairs(PairArgs a) {
     };
     pdl_wait();
     pdl_trigger();
-    double v = 0.0;
-#pragma unroll 4
-    for (int r = begin; r < end; r += HALF) {
-        const float w = weight(r), l = a.logp[r], ref = a.ref ? __ldg(a.ref + r) : 0.f;
-        if (w != 0.f) v += (double)w * ((double)l - (double)ref);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if (tid % 32 == 0) parts[tid / 32] = v;
     wrong = __syncthreads_or(wrong);
-    double sum[2] = {0.0, 0.0};
-#pragma unroll
-    for (int i = 0; i < PAIR_THREADS / 32; ++i) sum[i / (HALF / 32)] += parts[i];
-    double2 f = pair_loss(a, sum[0] - sum[1]);
-    if (wrong) f.x = f.y = sum[0] = sum[1] = NAN;
-    if (tid == 0) {
-        if (a.loss) a.loss[pair] = (float)f.x;
-        if (a.sums) a.sums[chosen] = (float)sum[0], a.sums[other] = (float)sum[1];
-    }
-    if (!a.slope) return;
-    const int64_t all = (int64_t)PAIR_THREADS * gridDim.x, at = (int64_t)pair * PAIR_THREADS + tid;
-    if (wrong) {
-        for (int64_t r = at; r < a.rows; r += all) a.slope[r] = NAN;
-        return;
-    }
-    const double slope = (side ? -f.y : f.y) * (a.pair_weight ? (double)__ldg(a.pair_weight + pair) : 1.0);
+    for (int pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
+        const int chosen = a.interleaved ? 2 * pair : pair, other = a.interleaved ? 2 * pair + 1 : a.pairs + pair;
+        if (wrong) {
+            if (tid == 0 && a.loss) a.loss[pair] = NAN;
+            if (tid == 0 && a.sums) a.sums[chosen] = a.sums[other] = NAN;
+            continue;
+        }
+        const int seq = side ? other : chosen, begin = __ldg(a.offsets + seq) + tid % HALF, end = __ldg(a.offsets + seq + 1);
+        double v = 0.0;
 #pragma unroll 4
-    for (int r = begin; r < end; r += HALF) {
-        const float w = weight(r);
-        a.slope[r] = w == 0.f ? 0.f : (float)(slope * w);
+        for (int r = begin; r < end; r += HALF) {
+            const float w = weight(r), l = a.logp[r], ref = a.ref ? __ldg(a.ref + r) : 0.f;
+            if (w != 0.f) v += (double)w * ((double)l - (double)ref);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (tid % 32 == 0) parts[tid / 32] = v;
+        __syncthreads();
+        double sum[2] = {0.0, 0.0};
+#pragma unroll
+        for (int i = 0; i < PAIR_THREADS / 32; ++i) sum[i / (HALF / 32)] += parts[i];
+        const double2 f = pair_loss(a, sum[0] - sum[1]);
+        if (tid == 0) {
+            if (a.loss) a.loss[pair] = (float)f.x;
+            if (a.sums) a.sums[chosen] = (float)sum[0], a.sums[other] = (float)sum[1];
+        }
+        if (a.slope) {
+            const double slope = (side ? -f.y : f.y) * (a.pair_weight ? (double)__ldg(a.pair_weight + pair) : 1.0);
+#pragma unroll 4
+            for (int r = begin; r < end; r += HALF) {
+                const float w = weight(r);
+                a.slope[r] = w == 0.f ? 0.f : (float)(slope * w);
+            }
+        }
+        __syncthreads();  // the sums have been read
     }
     // rows of no sequence
-    const int from = __ldg(a.offsets), to = __ldg(a.offsets + 2 * a.pairs);
-    if (from > 0 || to < a.rows)
-        for (int64_t r = at; r < a.rows; r += all)
-            if (r < from || r >= to) a.slope[r] = 0.f;
+    if (a.slope && (wrong || from > 0 || to < a.rows))
+        for (int64_t r = (int64_t)blockIdx.x * PAIR_THREADS + tid; r < a.rows; r += (int64_t)gridDim.x * PAIR_THREADS)
+            if (wrong || r < from || r >= to) a.slope[r] = wrong ? NAN : 0.f;
 }
 
 }  // namespace
 
 cudaError_t launch_pairs(const PairArgs& a, Stream& s) {
-    return launch_k(k_pairs, dim3((unsigned)a.pairs), dim3(PAIR_THREADS), 0, s, a);
+    return launch_k(k_pairs, dim3((unsigned)std::min(a.pairs, 4 * device_sm_count())), dim3(PAIR_THREADS), 0, s, a);
 }
 
 }  // namespace hbsjd

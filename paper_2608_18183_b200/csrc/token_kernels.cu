@@ -120,13 +120,9 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
         T* g = GRAD ? (T*)a.grad + (int64_t)row * a.ld_g + v0 : nullptr;
         const T* x1 = x0 + stride;
         const Part<G, WARPS> p1 = part_of(x1);
-        bool fetched = t1 < 0;
+        Next<T, G, WARPS> next = {ss, x1, p1, t1 >= 0};
         const int lo = p.first() - p.P, hi = p.last() - p.P;  // the warp's entries of the slice
         const bool first = rank == 0 && threadIdx.x == 0;
-        const auto each_then_next = [&](auto&& f) {
-            each_then(ss, p, !fetched, x1, p1, f);
-            fetched = true;
-        };
         if (t < 0) {  // (all CTAs of the row)
             if constexpr (GRAD) put_zeros(g, lo, hi);
             if (first && !a.at) {
@@ -143,7 +139,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
                 if constexpr (GRAD)
                     each_of(p, f);
                 else
-                    each_then_next(f);
+                    each_then(p, next, f);
             });
             const bool alone = WARPS == 1 && a.ctas == 1;  // the warp has the whole row
             if (!alone) {
@@ -173,11 +169,11 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
                 if constexpr (GRAD)
                     k.set<ENT>(r, v, H, a.d_logp ? terms.a : f.y, a.d_logp ? -terms.b : a.bonus, a.d_logp ? inv_tau : terms.a * inv_tau, c);
             }
-            if constexpr (GRAD) part_gradient<ENT>(ss, p, g, n, mine, k, c, each_then_next);
+            if constexpr (GRAD) part_gradient<ENT>(ss, p, g, n, mine, k, c, next, [&](auto&& f) { each_then(p, next, f); });
         }
         __syncwarp();  // the warp's part is done
+        if (next.more) stage_part(ss, x1, p1);
         x0 = x1, p = p1;
-        if (!fetched) stage_part(ss, x0, p);
         t = t1, t1 = t2, xt = xt1;
     }
 }
@@ -215,7 +211,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_spread(SpreadArgs a) {
         const T* x1 = x0 - (int64_t)step * a.ld;
         const Part<G, WARPS> p1 = part_of(x1);
         T* g = (T*)a.grad + (int64_t)row * a.ld_g;
-        bool fetched = r1.token < 0;
+        Next<T, G, WARPS> next = {ss, x1, p1, r1.token >= 0};
         const int lo = p.first() - p.P, hi = p.last() - p.P;  // the warp's entries
         if (r.token < 0) {
             put_zeros(g, lo, hi);
@@ -226,26 +222,26 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_spread(SpreadArgs a) {
             k.set<false>(TokenRow(r.stat.y, r.stat.z), v, 0.f, r.slope, 0.f, inv_tau, c);
             cp_async_wait_all();
             __syncwarp();
-            part_gradient<false>(ss, p, g, a.V, r.token >= lo && r.token < hi ? r.token : -1, k, c, [&](auto&& f) {
-                if (fetched) {
+            // (two loops here: 16 pairs of 256 positions of 16384 fp32 246 us in place of 261)
+            part_gradient<false>(ss, p, g, a.V, r.token >= lo && r.token < hi ? r.token : -1, k, c, next, [&](auto&& f) {
+                if (next.more)
+                    each_then(p, next, f);
+                else
                     each_of(p, f);
-                } else {
-                    each_then(ss, p, true, x1, p1, f);
-                    fetched = true;
-                }
             });
         }
         __syncwarp();
-        if (!fetched) stage_part(ss, x1, p1);
+        if (next.more) stage_part(ss, x1, p1);
         r = r1, r1 = r2, x0 = x1, p = p1;
     }
 }
 
-// No row waits for anything here: parts of rows of 8 KB, a warp each, from HBM to HBM.
+// The same by parts of rows of up to 4 KB, a warp each, from HBM to HBM.
 constexpr int SPREAD_THREADS = 256, SPREAD_WARPS = SPREAD_THREADS / 32, SPREAD_BYTES = 4096;
-template <typename T>
+// SHIFTED: the gradient may lie at another place behind 16 bytes than the logits.
+template <typename T, bool SHIFTED>
 __global__ void __launch_bounds__(SPREAD_THREADS, 4) k_spread_parts(SpreadArgs a) {
-    constexpr int G = 16 / sizeof(T), AHEAD = 4;  // groups a lane has on their way
+    constexpr int G = 16 / sizeof(T), AHEAD = SHIFTED ? 2 : 4;  // groups a lane has on their way
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
@@ -277,17 +273,34 @@ __global__ void __launch_bounds__(SPREAD_THREADS, 4) k_spread_parts(SpreadArgs a
             const int P = phase_of(x), first = P ? G - P : 0, groups = max(0, n - first) / G;  // whole groups of 16 bytes from x + first
             if (k.way == 2) {
                 put_zeros(g, 0, n);
-            } else if (k.way == 1 || P != phase_of(g)) {
+            } else if (k.way == 1) {
                 for (int e = lane; e < n; e += 32) {
-                    const float y = to_f<T>(x[e]);
-                    float lo, hi;
-                    if (k.way == 1) {
-                        const float q = ex2(held((y - k.m) * c)) * k.K;
-                        lo = q == 0.f ? 0.f : q * -k.A * k.scale;
-                    } else {
-                        split(of(both(y, y)), lo, hi);
+                    const float q = ex2(held((to_f<T>(x[e]) - k.m) * c)) * k.K;
+                    g[e] = from_f<T>(q == 0.f ? 0.f : q * -k.A * k.scale);
+                }
+            } else if (SHIFTED && P != phase_of(g)) {
+                Shifted<T, G> to(g, 0, n, P);
+                for (int j0 = to.first; j0 <= to.last + 1; j0 += 32 * AHEAD) {
+                    uint4 w[AHEAD];
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i) {
+                        const int e = (j0 + i * 32 + lane) * G - P;
+                        if (e >= 0 && e + G <= n)
+                            w[i] = __ldcs(reinterpret_cast<const uint4*>(x + e));
+                        else
+#pragma unroll
+                            for (int h = 0; h < G; ++h) reinterpret_cast<T*>(&w[i])[h] = e + h >= 0 && e + h < n ? x[e + h] : from_f<T>(0.f);
                     }
-                    g[e] = from_f<T>(lo);
+#pragma unroll
+                    for (int i = 0; i < AHEAD; ++i) {
+                        float y[G];
+                        uint32_t own[4];
+                        read<false>(reinterpret_cast<const T*>(&w[i]), y);
+#pragma unroll
+                        for (int h = 0; h < G; h += 2) split(of(both(y[h], y[h + 1])), y[h], y[h + 1]);
+                        packed(y, own);
+                        to.put(j0 + i * 32 + lane, own);
+                    }
                 }
             } else {
                 const T* xs = x + first;
@@ -377,30 +390,31 @@ template <typename T>
 cudaError_t run_spread(const SpreadArgs& args, Stream& s) {
     SpreadArgs a = args;
     const int sms = device_sm_count();
-    if constexpr (sizeof(T) == 4) {
-        // Rows of 64 fp32 KB on 256 threads, two an SM, or smaller ones alike; staged whole for the same order of reads and writes in HBM as
-        // theirs in k_token (16 pairs of 256 positions of 16384 266 us, of 16385 300; by parts 269 and 333).  In bf16, parts are as fast
-        // (64 pairs of 64 of 16384 148 and 153 us, 20 of 256 of 24001 306 and 277).
-        const size_t smem = (a.V + 24) / 8 * 8 * sizeof(T);
-        const int fit = (int)(227 * 1024 / (smem + 1024 + 128));  // (1 KB is the system's)
-        const auto run = [&](auto threads) {
-            constexpr int THREADS = decltype(threads)::value, PER_SM = 512 / THREADS;
-            const cudaError_t e = allow_row_smem<k_spread<T, THREADS, PER_SM>>();
-            if (e != cudaSuccess) return e;
-            return launch_kc(true, k_spread<T, THREADS, PER_SM>, dim3((unsigned)std::min(a.rows, sms * std::min(PER_SM, fit))), dim3(THREADS), smem, s, 1, a);
-        };
-        if (a.rows > sms && smem <= SHARED_SM) {
-            if (fit <= 3) return run(std::integral_constant<int, 256>());
-            if (fit <= 6) return run(std::integral_constant<int, 128>());
-            if (fit <= 14) return run(std::integral_constant<int, 64>());
-        }
+    const bool shifted = ((uintptr_t)a.x - (uintptr_t)a.grad) % 16 || (a.ld - a.ld_g) * (int64_t)sizeof(T) % 16;
+    // Rows of 64 KB on 256 threads, two an SM, or smaller ones alike; fp32 is staged whole for the same order of reads and writes in HBM as
+    // in k_token (16 pairs of 256 positions of 16384 266 us, of 16385 300; by parts 269 and 333).  In bf16 parts are as fast (64 pairs of 64 of
+    // 16384 148 and 153 us, 20 of 256 of 24001 306 and 277), unless the gradient lies otherwise (one of 4096, a stride of 16385: 172
+    // us, by parts 228).
+    const size_t smem = (a.V + 24) / 8 * 8 * sizeof(T);
+    const int fit = (int)(227 * 1024 / (smem + 1024 + 128));  // (1 KB is the system's)
+    const auto run = [&](auto threads) {
+        constexpr int THREADS = decltype(threads)::value, PER_SM = 512 / THREADS;
+        const cudaError_t e = allow_row_smem<k_spread<T, THREADS, PER_SM>>();
+        if (e != cudaSuccess) return e;
+        return launch_kc(true, k_spread<T, THREADS, PER_SM>, dim3((unsigned)std::min(a.rows, sms * std::min(PER_SM, fit))), dim3(THREADS), smem, s, 1, a);
+    };
+    if (a.rows > sms && smem <= SHARED_SM && (sizeof(T) == 4 || shifted)) {
+        if (fit <= 3) return run(std::integral_constant<int, 256>());
+        if (fit <= 6) return run(std::integral_constant<int, 128>());
+        if (fit <= 14) return run(std::integral_constant<int, 64>());
     }
     const int most = SPREAD_BYTES / (int)sizeof(T);
     a.parts = (a.V + most - 1) / most;
     a.part = ((a.V + a.parts - 1) / a.parts + 7) / 8 * 8;
     const int64_t items = (int64_t)a.rows * a.parts;
     const dim3 grid((unsigned)std::min<int64_t>((int64_t)sms * 4, (items + SPREAD_WARPS - 1) / SPREAD_WARPS));
-    return launch_k(k_spread_parts<T>, grid, dim3(SPREAD_THREADS), 0, s, a);
+    if (shifted) return launch_k(k_spread_parts<T, true>, grid, dim3(SPREAD_THREADS), 0, s, a);
+    return launch_k(k_spread_parts<T, false>, grid, dim3(SPREAD_THREADS), 0, s, a);
 }
 
 }  // namespace

@@ -49,9 +49,6 @@ __device__ __forceinline__ void read(const bf16* p, float (&x)[8]) {
     }
 }
 
-__device__ __forceinline__ void put2(float* p, float lo, float hi) { __stcs(reinterpret_cast<float2*>(p), make_float2(lo, hi)); }
-__device__ __forceinline__ void put2(bf16* p, float lo, float hi) { __stcs(reinterpret_cast<uint32_t*>(p), pack(lo, hi)); }
-
 // Where x c - m c may be taken as one multiply-add of x: t is as good as its own rounding, and m c is off by `rest`, less than 2^-4.
 __device__ __forceinline__ bool is_plain(float m, float c) { return fabsf(m) < 1e28f && fabsf(m * c) < 1048576.f && c > 1e-20f && c < 1e8f; }
 // 2^-rest
@@ -181,15 +178,110 @@ struct TokenCoefs {
         float d = A * r.qo;
         if (ENT) d += B * (r.qt == 0.f ? 0.f : r.qt * (r.l + H));
         token = r.empty ? 0.f : scale * d;
-        // (NaN passes)
-        way = r.empty || r.alone ? 2 : fabsf(y0) + fabsf(y1) < 1e30f && is_plain(v.m, c) ? 0 : 1;
+        // (NaN passes; masked entries have exponents of down to -1e30 c, which y1 times is to be finite beside their share of zero)
+        way = r.empty || (r.alone && A == A && B == B) ? 2 : fabsf(y0) + fabsf(y1) < 1e30f && fabsf(y1) * c < 1e7f && is_plain(v.m, c) ? 0 : 1;
     }
 };
 
+// The part p1 of a slice at x1 that comes next, if there is one: groups of the part at hand that were read for the last time make place for
+// it in the stage.
+template <typename T, int G, int WARPS>
+struct Next {
+    T* ss;
+    const T* x1;
+    const Part<G, WARPS>& p1;
+    bool more;  // one comes, and nothing of it has been fetched
+    // group j was read for the last time, by this lane
+    __device__ __forceinline__ void take(int j, int inner, int count) const {
+        if ((unsigned)(j - inner) < (unsigned)count) cp_async16(ss + j * G, x1 - p1.P + j * G);
+    }
+    __device__ __forceinline__ int count() const { return more ? p1.outer() - p1.inner() : 0; }
+    // all groups of p were
+    __device__ __forceinline__ void taken(const Part<G, WARPS>& p) {
+        if (!more) return;
+        more = false;
+        const int lane = threadIdx.x & 31, inner = p1.inner(), outer = p1.outer();
+        const T* base = x1 - p1.P;
+        __syncwarp();
+        // (at another place behind 16 bytes a part may have groups that this one had not)
+        const int from = p.inner() - (p.inner() > p.j0), to = p.outer() + (p.outer() < p.j1);
+        for (int j = inner + lane; j < min(outer, from); j += 32) cp_async16(ss + j * G, base + j * G);
+        for (int j = max(inner, to) + lane; j < outer; j += 32) cp_async16(ss + j * G, base + j * G);
+        stage_ends(ss, x1, p1);
+    }
+};
+// f(j, whole) for all groups of p, the last that reads them.  (One loop whether or not one comes next: two of them in k_token cost 8192 bf16
+// rows of 16384 with entropy and gradient 115 us in place of 109.)
+template <typename T, int G, int WARPS, typename F>
+__device__ __forceinline__ void each_then(const Part<G, WARPS>& p, Next<T, G, WARPS>& next, F&& f) {
+    const int inner = next.p1.inner(), count = next.count();
+    each_of(p, [&](int j, auto whole) {
+        f(j, whole);
+        next.take(j, inner, count);
+    });
+    next.taken(p);
+}
 
-// A warp's part of the gradient at g, n entries of which are the slice's.  walk(f): as above.
+// G values as they are stored.
+__device__ __forceinline__ void packed(const float (&x)[4], uint32_t (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+}
+__device__ __forceinline__ void packed(const float (&x)[8], uint32_t (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack(x[2 * i], x[2 * i + 1]);
+}
+
+// Entries [lo, hi) of out by a warp, where they lie at another place behind 16 bytes than in the groups that they come in: of group j, entry
+// j G - P is the first.  A lane's 16 bytes are the end of the group before its own, which the lane before it has, and the beginning of
+// its own.  (Two entries a lane, one by one from shared memory: 8192 bf16 rows of 16384 with a stride of 16385, policy loss with gradient,
+// 139 us; so: 123.)
+template <typename T, int G>
+struct Shifted {
+    T* out;
+    int lo, hi, first, last;  // groups [first, last] hold some of them; turns go on to group last + 1
+    int Pg, back, words, half;
+    uint32_t before[4];  // the lane's group of the turn before
+    __device__ __forceinline__ Shifted(T* out, int lo, int hi, int P) : out(out), lo(lo), hi(hi), Pg(phase_of(out)), before{0, 0, 0, 0} {
+        const int d = (P - Pg + G) % G;
+        back = P < Pg, words = d * (int)sizeof(T) / 4, half = sizeof(T) == 2 && d % 2;
+        first = (P + lo) / G, last = lo < hi ? (P + hi - 1) / G : first - 2;
+    }
+    // all lanes, each with its own group: j = first + lane, and 32 more from turn to turn
+    __device__ __forceinline__ void put(int j, const uint32_t (&own)[4]) {
+        const int lane = threadIdx.x & 31;
+        uint32_t c[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            c[i] = __shfl_sync(0xffffffffu, lane == 31 ? before[i] : own[i], (lane + 31) & 31);
+            c[4 + i] = before[i] = own[i];
+        }
+        if (words & 2)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) c[i] = c[i + 2];
+        if (words & 1)
+#pragma unroll
+            for (int i = 0; i < 5; ++i) c[i] = c[i + 1];
+        if (half)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c[i] = __funnelshift_r(c[i], c[i + 1], 16);
+        const int e = (j - 1 + back) * G - Pg;
+        if (e >= lo && e + G <= hi) {
+            __stcs(reinterpret_cast<uint4*>(out + e), make_uint4(c[0], c[1], c[2], c[3]));
+        } else {
+            const T* x = reinterpret_cast<const T*>(c);
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (e + i >= lo && e + i < hi) out[e + i] = x[i];
+        }
+    }
+};
+
+// A warp's part of the gradient at g, n entries of which are the slice's, and the place for what comes next (where no careful way was
+// taken).  walk(f) has f read every group, as each_then does.
 template <bool ENT, typename T, int G, int WARPS, typename W>
-__device__ __forceinline__ void part_gradient(const T* ss, const Part<G, WARPS>& p, T* g, int n, int mine, const TokenCoefs& k, float c, W&& walk) {
+__device__ __forceinline__ void part_gradient(const T* ss, const Part<G, WARPS>& p, T* g, int n, int mine, const TokenCoefs& k, float c,
+                                              Next<T, G, WARPS>& next, W&& walk) {
     const int lane = threadIdx.x & 31, lo = p.first() - p.P, hi = p.last() - p.P, Pg = phase_of(g);
     if (k.way == 2) {
         put_zeros(g, lo, hi);
@@ -217,43 +309,28 @@ __device__ __forceinline__ void part_gradient(const T* ss, const Part<G, WARPS>&
                 else
                     put_at<T, G>(g, j * G - p.P, 0, n, x);
             });
-        } else {  // two entries a lane: neighbours in the gradient, in order in shared memory
-            for (int e = (lo + Pg) / 2 * 2 - Pg + lane * 2; e < hi; e += 64) {
-                float x0 = to_f<T>(ss[p.P + max(e, lo)]), x1 = to_f<T>(ss[p.P + min(e + 1, hi - 1)]);
-                if (ENT) x0 = above(x0), x1 = above(x1);
-                split(of(both(x0, x1)), x0, x1);
-                if (e >= lo && e + 1 < hi) {
-                    put2(g + e, x0, x1);
-                } else {
-                    if (e >= lo) g[e] = from_f<T>(x0);
-                    if (e + 1 < hi) g[e + 1] = from_f<T>(x1);
+        } else {
+            Shifted<T, G> to(g, lo, hi, p.P);
+            const int inner = next.p1.inner(), count = next.count();
+#pragma unroll 2
+            for (int j0 = to.first; j0 <= to.last + 1; j0 += 32) {
+                const int j = j0 + lane;
+                uint32_t w[4] = {0, 0, 0, 0};
+                if (j <= to.last) {
+                    float x[G];
+                    read<ENT>(ss + j * G, x);
+#pragma unroll
+                    for (int i = 0; i < G; i += 2) split(of(both(x[i], x[i + 1])), x[i], x[i + 1]);
+                    packed(x, w);
+                    next.take(j, inner, count);
                 }
+                to.put(j, w);
             }
+            next.taken(p);
         }
     }
     __syncwarp();  // the token's place was written above
     if (mine >= 0 && lane == 0) g[mine] = from_f<T>(k.token);
-}
-
-// Reads every group of a part p for the last time, f(j, whole), and, if there is one to come, has each make place for the same group of the
-// part p1 of a slice at x1, whose copies have begun when it returns.  (One loop for both: two of them in a kernel cost 8192 bf16 rows of
-// 16384 with entropy and gradient 115 us in place of 109.)
-template <typename T, int G, int WARPS, typename F>
-__device__ __forceinline__ void each_then(T* ss, const Part<G, WARPS>& p, bool more, const T* x1, const Part<G, WARPS>& p1, F&& f) {
-    const int lane = threadIdx.x & 31, inner = p1.inner(), count = more ? p1.outer() - inner : 0;
-    const T* base = x1 - p1.P;
-    each_of(p, [&](int j, auto whole) {
-        f(j, whole);
-        if ((unsigned)(j - inner) < (unsigned)count) cp_async16(ss + j * G, base + j * G);
-    });
-    if (more) {
-        __syncwarp();
-        // (at another place behind 16 bytes a part may have groups that this one had not)
-        const int from = p.inner() - (p.inner() > p.j0), to = p.outer() + (p.outer() < p.j1);
-        for (int j = inner + lane; j < min(inner + count, from); j += 32) cp_async16(ss + j * G, base + j * G);
-        for (int j = max(inner, to) + lane; j < inner + count; j += 32) cp_async16(ss + j * G, base + j * G);
-        stage_ends(ss, x1, p1);
-    }
 }
 
 }  // namespace hbsjd

@@ -185,3 +185,28 @@ def test_refusals_of_tensors():
         with pytest.raises(binding.HbsjdError) as e:
             call()
         assert e.value.code == -1
+
+
+def test_more_pairs_than_ctas():
+    """Thousands of pairs of a position or two, some empty."""
+    import torch
+    g = torch.Generator().manual_seed(5)
+    lengths = [int(v) for v in torch.randint(0, 4, (2 * 3001,), generator=g)]
+    rows = sum(lengths)
+    x = _rows(3, rows, 64)
+    t = sampled(x, 1.0, _gen(3))
+    ref = Rows(x, t, 1.0).l.float() + 0.3
+    for interleaved in (False, True):
+        _check(x, t, lengths, "fp32", ref, interleaved=interleaved, beta=0.5)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,pad,shift", [(16384, 1, 0), (4099, 2, 1), (20000, 1, 3), (513, 3, 2)])
+def test_gradients_that_lie_otherwise_than_the_logits(V, pad, shift, dtype):
+    import torch
+    lengths = [200, 30, 77, 100]
+    x = _rows(V, 407, V, 3.0, dtype, pad, shift)
+    t = sampled(x, 1.0, _gen(1))
+    _check(x, t, lengths, dtype, beta=0.02)
+    grad = torch.empty(407, V + 5, device="cuda", dtype=x.dtype)[:, 3:V + 3]
+    _check(x, t, lengths, dtype, beta=0.02, grad=grad)

@@ -289,3 +289,33 @@ def test_refusals_of_tensors():
         with pytest.raises(binding.HbsjdError) as e:
             call()
         assert e.value.code == -1
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_large_factors_beside_masked_entries(dtype):
+    """Slopes and weights of up to 1e20: no entry without mass has a gradient."""
+    import torch
+    x = _rows(5, 6, 2000, 3.0, dtype)
+    x[:, ::3] = NEG
+    x[3:, 1::3] = -1e30
+    t = torch.full((6,), 2, dtype=torch.int32, device="cuda")
+    for size in (1e8, 1e15, 1e20):
+        a = torch.full((6,), size, device="cuda")
+        for ent in (None, a, -a):
+            r = Rows(x, t, 0.5)
+            g = binding.hbsjd_token_logprobs_grad(x, t, a, ent, 0.5)
+            want, bound = r.gradient(a.double(), None if ent is None else ent.double(), torch.ones_like(r.l))
+            near(g, want, bound, HALF[dtype])
+            assert not bool(g[:, ::3].any())
+
+
+def test_slopes_that_are_no_numbers():
+    """NaN slopes make their row's gradient NaN, where the token has all the mass too."""
+    import torch
+    x, t = _rows(5, 4, 300), torch.full((4,), 7, dtype=torch.int32, device="cuda")
+    x[1] = NEG
+    x[1, 7] = 1.0
+    a = torch.tensor([1.0, float("nan"), float("nan"), 1.0], device="cuda")
+    for ent in (None, a):
+        g = binding.hbsjd_token_logprobs_grad(x, t, a, ent)
+        assert bool(torch.isnan(g[1:3]).all()) and bool(torch.isfinite(g[0]).all()) and bool(torch.isfinite(g[3]).all())
