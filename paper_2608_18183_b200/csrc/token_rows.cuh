@@ -57,12 +57,14 @@ __device__ __forceinline__ float less(float rest) {
     return fmaf(y, fmaf(y, fmaf(y, 1.f / 6, 0.5f), 1.f), 1.f);
 }
 
-// ln z of a normal z, within 2^-22 and its own rounding: the power of two apart, so that lg2 has its absolute error.
-__device__ __forceinline__ float ln(float z) {
+// ln z of a normal z as a sum of two: the power of two apart, so that lg2 has its absolute error of 2^-22.  (A series for the rest, good to
+// 1e-9, leans to the other side, since ex2 does: 3e-8 a row of 16384 in place of 5e-9.)
+__device__ __forceinline__ float2 ln(float z) {
     const uint32_t b = __float_as_uint(z);
     // (zero, infinities and NaN as lg2 has them)
     const int k = b - 0x00800000u < 0x7f000000u ? (int)(b >> 23) - 127 : 0;
-    return LN2 * ((float)k + lg2(__uint_as_float(b - ((uint32_t)k << 23))));
+    const float f = LN2 * lg2(__uint_as_float(b - ((uint32_t)k << 23))), hi = (float)k * LN2;
+    return {hi, f + fmaf((float)k, LN2, -hi) - (float)k * 1.90465e-9f};  // (LN2 is that much above ln 2)
 }
 
 // log(1 + s), s in 0..1, to its own last digits: 2 (u + u^3 / 3 + u^5 / 5 ...) with u = s / (2 + s), which leaves 1e-8 of it behind u^15.
@@ -152,12 +154,17 @@ struct TokenRow {
         empty = v.z == 0.f && xt == -INFINITY;
         alone = v.z == 0.f && xt < INFINITY;
         // (an infinite logit: NaN)
-        const float lz = ln(v.z), D = xt < INFINITY ? fmaf(v.m - xt, inv_tau, lz) : NAN, s = ex2(-fabsf(D) * LOG2E);
+        // (D's parts are as large as l: what the rounding of their sum leaves is added before the next, so that l is about as good as its own)
+        const float2 lz = ln(v.z);
+        const float gap = v.m - xt, big = fmaf(gap, inv_tau, lz.x), rest = fmaf(gap, inv_tau, lz.x - big) + lz.y;
+        float D = big + lz.y;
+        if (!(xt < INFINITY)) D = NAN;
+        const float s = ex2(-fabsf(D) * LOG2E);
         const float share = __fdividef(1.f, 1.f + s);
         qo = D > 0.f ? share : s * share, qt = D > 0.f ? s * share : share;
         const float near = log1p_of(s);
-        l = -(near + fmaxf(D, 0.f));
-        Lk = lz + (near + fmaxf(-D, 0.f));
+        l = D > 0.f && D < INFINITY ? -(big + (rest + near)) : -(near + fmaxf(D, 0.f));
+        Lk = lz.x + (lz.y + (near + fmaxf(-D, 0.f)));
     }
     __device__ __forceinline__ float logp() const { return empty ? -INFINITY : l == 0.f ? 0.f : l; }
 };
