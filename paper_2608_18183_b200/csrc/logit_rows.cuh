@@ -524,8 +524,8 @@ struct TokenArgs {
     const float *d_logp, *d_entropy;          // [rows]: the gradient of these; null: the policy's, none
     float *loss, *logp, *entropy;             // [rows] or null
     void* grad;              // rows, or null
-    float4* stats;           // [rows] or null: m, z (see TokenSums), the mass of the others
-    int rows, V, ctas, slice;
+    float4* stats;           // [rows] or null: m, z (see TokenSums), the mass of the others, what the rounding of logp left
+    int rows, V, ctas, slice, summed;  // summed: logp is for sums over many rows
     float temperature, low, high, dual, kl, bonus;
     // rows of a scoring forward (see TopkArgs); tokens, logp and entropy are [batch][T] then
     const int2* at;
@@ -550,6 +550,7 @@ cudaError_t launch_spread(const SpreadArgs& a, int rows, int dtype, Stream& s);
 struct PairArgs {
     const int32_t *offsets, *tokens;  // [2 pairs + 1], [rows]
     const float *logp, *ref, *weight, *pair_weight;  // [rows], [rows] or null, [rows] or null, [pairs] or null
+    const float4* stats;     // [rows]
     float *loss, *sums;      // [pairs], [2 pairs]; null: not wanted
     float* slope;            // [rows] or null
     int rows, V, pairs, kind, interleaved;

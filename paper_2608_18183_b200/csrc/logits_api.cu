@@ -344,7 +344,8 @@ int hbsjd_preference_loss(void* cuda_stream, const hbsjd_preference_desc* d, con
     TokenArgs a = token_args(d, logits, tokens, nullptr);
     a.weight = weight;
     a.logp = logp ? logp : own;
-    a.stats = grad ? stats : nullptr;
+    a.stats = stats;
+    a.summed = 1;
     cudaError_t e = launch_token(a, d->rows, d->dtype, s);
     if (e != cudaSuccess) return launched(what, e);
     PairArgs p = {};
@@ -352,6 +353,7 @@ int hbsjd_preference_loss(void* cuda_stream, const hbsjd_preference_desc* d, con
     p.tokens = tokens;
     p.V = d->V;
     p.logp = a.logp;
+    p.stats = stats;
     p.ref = ref_logp;
     p.weight = weight;
     p.pair_weight = pair_weight;

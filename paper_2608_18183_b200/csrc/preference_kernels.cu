@@ -2,7 +2,7 @@
 //
 //   S_s = sum over the rows of sequence s of w (l - ref),  h = S_chosen - S_rejected,
 //   sigmoid: z = beta h - margin, (1 - e) log(1 + e^-z) + e log(1 + e^z);  hinge: max(0, 1 - z);  square: (h - 1 / (2 beta))^2.
-// The sums are in 64 bits: h is a difference of sums over hundreds of rows, small beside them.
+// The sums are in 64 bits, and l comes with what its rounding left: h is a difference of sums over hundreds of rows, small beside them.
 #include "../../include/hbsjd.h"
 #include "logit_rows.cuh"
 
@@ -58,8 +58,8 @@ __global__ void __launch_bounds__(PAIR_THREADS) k_pairs(PairArgs a) {
         double v = 0.0;
 #pragma unroll 4
         for (int r = begin; r < end; r += HALF) {
-            const float w = weight(r), l = a.logp[r], ref = a.ref ? __ldg(a.ref + r) : 0.f;
-            if (w != 0.f) v += (double)w * ((double)l - (double)ref);
+            const float w = weight(r), l = a.logp[r], low = a.stats[r].w, ref = a.ref ? __ldg(a.ref + r) : 0.f;
+            if (w != 0.f) v += (double)w * (((double)l - (double)ref) + (double)low);
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
             TokenCoefs k;
             if (GRAD || wid == 0) {  // (each warp for itself: one for all, and a barrier, cost 16384 rows of 16384 365 us in place of 351)
                 if (!alone) v = collect_sums<ENT>(slots + (parity ^ 1) * places, places, c);
-                const TokenRow r(v, xt, inv_tau);
+                const TokenRow r(v, xt, inv_tau, !GRAD && a.summed);
                 float H = 0.f;
                 if (ENT && !r.empty) H = (v.z == 0.f || r.qo == 0.f ? 0.f : r.qo * (r.Lk - LN2 * __fdividef(v.a, v.z))) - (r.qt == 0.f ? 0.f : r.qt * r.l);
                 float2 f = {0.f, 0.f};
@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
                     if (a.loss) a.loss[row] = r.empty ? 0.f : a.bonus != 0.f ? fmaf(-a.bonus, H, f.x) : f.x;
                     if (a.logp) a.logp[place] = r.logp();
                     if (ENT && a.entropy) a.entropy[place] = H;
-                    if (!GRAD && a.stats) a.stats[row] = make_float4(v.m, v.z, r.empty ? 0.f : r.qo, 0.f);
+                    if (!GRAD && a.stats) a.stats[row] = make_float4(v.m, v.z, r.empty ? 0.f : r.qo, r.empty ? 0.f : r.low);
                 }
                 if constexpr (GRAD)
                     k.set<ENT>(r, v, H, a.d_logp ? terms.a : f.y, a.d_logp ? -terms.b : a.bonus, a.d_logp ? inv_tau : terms.a * inv_tau, c);

@@ -57,14 +57,24 @@ __device__ __forceinline__ float less(float rest) {
     return fmaf(y, fmaf(y, fmaf(y, 1.f / 6, 0.5f), 1.f), 1.f);
 }
 
-// ln z of a normal z as a sum of two: the power of two apart, so that lg2 has its absolute error of 2^-22.  (A series for the rest, good to
-// 1e-9, leans to the other side, since ex2 does: 3e-8 a row of 16384 in place of 5e-9.)
+// ln z of a normal z as a sum of two: the power of two apart, so that lg2 has its absolute error of 2^-22.
 __device__ __forceinline__ float2 ln(float z) {
     const uint32_t b = __float_as_uint(z);
     // (zero, infinities and NaN as lg2 has them)
     const int k = b - 0x00800000u < 0x7f000000u ? (int)(b >> 23) - 127 : 0;
     const float f = LN2 * lg2(__uint_as_float(b - ((uint32_t)k << 23))), hi = (float)k * LN2;
     return {hi, f + fmaf((float)k, LN2, -hi) - (float)k * 1.90465e-9f};  // (LN2 is that much above ln 2)
+}
+// The same for sums over many rows, where what all rows are off alike adds up (lg2 leaves up to 2e-8 a row, by its argument): z = 2^k f with
+// f in [sqrt 1/2, sqrt 2), and ln f = 2 (u + u^3 / 3 + u^5 / 5 ...) with u = (f - 1) / (f + 1), which leaves 1e-9 behind u^9; and the 2e-8 that sums of
+// ex2 were below their exact ones (1e-8 of 1000 entries, 3e-8 of 16384).
+__device__ __forceinline__ float2 ln_without_lean(float z) {
+    const int b = __float_as_int(z);
+    if ((uint32_t)(b - 0x00800000) >= 0x7f000000u) return ln(z);  // zero, infinities and NaN
+    const int k = (b - 0x3f3504f3) >> 23;  // (sqrt 1/2)
+    const float f = __int_as_float(b - (k << 23)), u = __fdividef(f - 1.f, f + 1.f), u2 = u * u;
+    const float g = 2.f * u * fmaf(u2, fmaf(u2, fmaf(u2, fmaf(u2, 1.f / 9, 1.f / 7), 0.2f), 1.f / 3), 1.f), hi = (float)k * LN2;
+    return {hi, g + (fmaf((float)k, LN2, -hi) - (float)k * 1.90465e-9f + 2e-8f)};
 }
 
 // log(1 + s), s in 0..1, to its own last digits: 2 (u + u^3 / 3 + u^5 / 5 ...) with u = s / (2 + s), which leaves 1e-8 of it behind u^15.
@@ -147,23 +157,30 @@ struct TokenRow {
     bool alone;      // the token alone has
     float l, qo, qt; // log q of the token, masses of the others and of the token
     float Lk;        // log q_v = ln2 t_v - Lk
+    float low;       // what l's own rounding left, if asked for
     // of what was kept of one
-    __device__ __forceinline__ TokenRow(float z, float others) : empty(false), alone(z == 0.f && others == 0.f), l(0.f), qo(others), qt(0.f), Lk(0.f) {}
-    __device__ __forceinline__ TokenRow() {}
-    __device__ __forceinline__ TokenRow(const TokenSums& v, float xt, float inv_tau) {
+    __device__ __forceinline__ TokenRow(float z, float others) : empty(false), alone(z == 0.f && others == 0.f), l(0.f), qo(others), qt(0.f), Lk(0.f), low(0.f) {}
+    // summed: l and low are for sums over many rows
+    __device__ __forceinline__ TokenRow(const TokenSums& v, float xt, float inv_tau, bool summed) {
         empty = v.z == 0.f && xt == -INFINITY;
         alone = v.z == 0.f && xt < INFINITY;
         // (an infinite logit: NaN)
         // (D's parts are as large as l: what the rounding of their sum leaves is added before the next, so that l is about as good as its own)
-        const float2 lz = ln(v.z);
-        const float gap = v.m - xt, big = fmaf(gap, inv_tau, lz.x), rest = fmaf(gap, inv_tau, lz.x - big) + lz.y;
-        float D = big + lz.y;
+        const float2 lz = summed ? ln_without_lean(v.z) : ln(v.z);
+        const float gap = v.m - xt, big = fmaf(gap, inv_tau, lz.x);
+        float rest = fmaf(gap, inv_tau, lz.x - big) + lz.y, D = big + lz.y;
         if (!(xt < INFINITY)) D = NAN;
         const float s = ex2(-fabsf(D) * LOG2E);
         const float share = __fdividef(1.f, 1.f + s);
         qo = D > 0.f ? share : s * share, qt = D > 0.f ? s * share : share;
         const float near = log1p_of(s);
+        if (summed) {  // all that the roundings left
+            const float back = gap - v.m, off = (v.m - (gap - back)) - (xt + back), p = gap * inv_tau, t = big - p;
+            rest = (p - (big - t)) + (lz.x - t) + (fmaf(gap, inv_tau, -p) + off * inv_tau) + lz.y;
+        }
         l = D > 0.f && D < INFINITY ? -(big + (rest + near)) : -(near + fmaxf(D, 0.f));
+        low = summed && D > 0.f ? -((big + l) + (rest + near)) : 0.f;
+        if (!(fabsf(low) < 1.f)) low = 0.f;
         Lk = lz.x + (lz.y + (near + fmaxf(-D, 0.f)));
     }
     __device__ __forceinline__ float logp() const { return empty ? -INFINITY : l == 0.f ? 0.f : l; }
