@@ -432,9 +432,9 @@ int hbsjd_distill_topk(void *cuda_stream, const hbsjd_distill_desc *d, const voi
 
 /* ---- training by rewards and preferences -----------------------------------------------------------------------------------
  * The on-policy step without a teacher: log-probabilities of the sampled tokens, losses on them with their gradients, and the
- * clipping of the gradients that they end in.  The conventions are those of the operators on rows of logits, with x = logits /
- * temperature and q = softmax(x); tokens are int32 [rows], and one outside 0..V-1 leaves its row out: it is not read, its outputs are
- * 0 and its gradient zeros.  An entry of -inf has no mass; NaN and +inf make what their row gives NaN.
+ * clipping of the gradients that they end in.  The conventions are those of the operators on rows of logits (but where more
+ * kernels or a workspace are named), with x = logits / temperature and q = softmax(x); tokens are int32 [rows], and one
+ * outside 0..V-1 leaves its row out: it is not read, its outputs are 0 and its gradient zeros.  An entry of -inf has no mass; NaN and +inf make what their row gives NaN.
  *
  * hbsjd_token_logprobs: logp[r] = log q_token (-inf: no mass), entropy[r] = -sum q log q;  fp32 [rows], either may be NULL.  A row
  *   without mass: -inf and 0.
@@ -490,7 +490,7 @@ int hbsjd_policy_loss(void *cuda_stream, const hbsjd_policy_desc *d, const void 
  *   loss fp32 [pairs] or NULL;  sums fp32 [2 pairs] or NULL: S_s;  logp fp32 [rows] or NULL: log q_token (0: left out)
  *   grad [rows, V] or NULL: zeros for rows of no sequence
  *   workspace hbsjd_preference_workspace(d) bytes, aligned to 16, which no other call uses at the same time; whatever it holds
- * smoothing in 0..1 and margin are 0 where the loss has none; beta > 0.  Launches several kernels. */
+ * smoothing in 0..1 and margin are 0 where the loss has none; beta > 0.  Launches three kernels. */
 enum { HBSJD_PREFERENCE_SIGMOID = 0, HBSJD_PREFERENCE_HINGE = 1, HBSJD_PREFERENCE_SQUARE = 2 };
 typedef struct {
     int32_t rows, V, dtype, pairs, kind, interleaved;

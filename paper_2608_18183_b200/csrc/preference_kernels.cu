@@ -3,6 +3,12 @@
 //   S_s = sum over the rows of sequence s of w (l - ref),  h = S_chosen - S_rejected,
 //   sigmoid: z = beta h - margin, (1 - e) log(1 + e^-z) + e log(1 + e^z);  hinge: max(0, 1 - z);  square: (h - 1 / (2 beta))^2.
 // The sums are in 64 bits, and l comes with what its rounding left: h is a difference of sums over hundreds of rows, small beside them.
+//
+// A row's gradient needs its whole pair's sums, so the call is three kernels: k_token sums over the rows and keeps 16 bytes of each, k_pairs (here,
+// 5 us of latencies) makes the slopes, k_spread writes the gradient from what was kept, reading the logits a second time, the last rows
+// first.  That second reading is what bounds it: 16 pairs of 256 positions of 16384 fp32 250 us, where two readings and a writing take 229 at a
+// copy's rate (one reading 156).  L2 does not save it: a pair is 33 MB there, and gradients some rows behind the sums, in one kernel, still read 0.92
+// of all logits twice (350 us); batches of fewer pairs a launch pay 5 us of ramp each.
 #include "../../include/hbsjd.h"
 #include "logit_rows.cuh"
 

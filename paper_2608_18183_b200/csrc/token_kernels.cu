@@ -1,6 +1,14 @@
-// Log-probabilities of sampled tokens, the clipped policy loss and what both give back to the logits, in one pass over memory.
-// (see token_rows.cuh for the formulas).  Two sums over a row (exponentials, and weighted by their exponents where the entropy is wanted)
-// give the loss, and a second look at the row the gradient.
+// Log-probabilities of sampled tokens, the clipped policy loss and what both give back to the logits, in one pass over memory (see
+// token_rows.cuh for the formulas).
+//
+// Two sums over a row (exponentials, and weighted by their exponents where the entropy is wanted) give the loss, and a second look at the row
+// the gradient.  In between the row stays in shared memory: it is read from HBM once and the gradient written once, which bounds fp32; in bf16
+// the two exponentials an entry and about 18 instructions (a third of them what a warp does once a row) share the time with it.  Rows are
+// dealt to resident CTAs; a warp has a part of each to itself, as in the divergences, meets the others for the sums alone, and fetches its part of the
+// next row group by group as it reads this one for the last time, wherever that row lies behind 16 bytes.  Long rows, and few, are split over a
+// cluster.  Measured, the kernel alone: log-probabilities and entropies of 8192 rows of 16384 fp32 88 us (0.94 of a copy's rate); policy
+// loss with gradient of 16384 such rows, an eighth left out, 327 us (0.95); with entropy, 8192 rows in bf16 110 us (0.75); backward of 3001 rows of 24001 bf16 70 us
+// (0.64: rows that begin anywhere in a line cost a quarter more requests).
 #include <type_traits>
 
 #include "token_rows.cuh"

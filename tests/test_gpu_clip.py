@@ -202,3 +202,15 @@ def test_streams_graphs_and_autograd():
     assert [x._version for x in g] == before
     binding.hbsjd_clip_gradients(g, 1.0)
     assert all(x._version > b for x, b in zip(g, before))
+
+
+def test_an_array_beyond_32_bits():
+    import torch
+    n = 2 ** 31 + 12345
+    x = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    x[-1], x[0], x[2 ** 31 + 1] = 3.0, 4.0, 12.0
+    y = torch.full((77,), 0.0, device="cuda")
+    norm = binding.hbsjd_clip_gradients([y, x], 1.3)
+    assert float(norm) == 13.0
+    assert [float(x[i]) for i in (-1, 0, 2 ** 31 + 1)] == [float(torch.tensor(v * 0.1 / (1 + 1e-6 / 13)).bfloat16()) for v in (3.0, 4.0, 12.0)]
+    assert int(torch.count_nonzero(x)) == 3

@@ -319,3 +319,27 @@ def test_slopes_that_are_no_numbers():
     for ent in (None, a):
         g = binding.hbsjd_token_logprobs_grad(x, t, a, ent)
         assert bool(torch.isnan(g[1:3]).all()) and bool(torch.isfinite(g[0]).all()) and bool(torch.isfinite(g[3]).all())
+
+
+def test_places_beyond_32_bits():
+    """More than 2^32 bytes and 2^31 entries of logits: the last rows are as they are alone."""
+    import torch
+    rows, V = 132000, 16384
+    x = torch.zeros(rows, V, dtype=torch.bfloat16, device="cuda")
+    t = torch.randint(0, V, (rows,), generator=_gen(1), device="cuda").int()
+    x[-300:] = _rows(2, 300, V, 3.0, "bf16")
+    A = torch.randn(rows, generator=_gen(3), device="cuda")
+    loss, g, logp, _ = binding.hbsjd_policy_loss(x, t, A, entropy=0.01)
+    alone = binding.hbsjd_policy_loss(x[-300:], t[-300:], A[-300:], entropy=0.01)
+    # (other CTAs, other orders of a row's sums)
+    torch.testing.assert_close(loss[-300:], alone[0], rtol=1e-5, atol=1e-6)
+    torch.testing.assert_close(logp[-300:], alone[2], rtol=1e-5, atol=1e-6)
+    torch.testing.assert_close(g[-300:].float(), alone[1].float(), rtol=1e-2, atol=1e-9)
+    flat = torch.tensor(V, device="cuda").double().log()
+    near(logp[:-300], -flat.expand(rows - 300), torch.full_like(logp[:-300], 2e-5).double(), HALF["fp32"])
+    offsets = torch.tensor([0, rows - 300, rows - 150, rows - 150, rows], device="cuda").int()
+    small = torch.tensor([0, 0, 150, 150, 300], device="cuda").int()
+    _, g2, sums = binding.hbsjd_preference_loss(x, t, offsets, beta=1e-4, grad=g)
+    _, want, wsums = binding.hbsjd_preference_loss(x[-300:], t[-300:], small, beta=1e-4)
+    torch.testing.assert_close(sums[1:], wsums[1:], rtol=1e-5, atol=1e-4)
+    assert bool(torch.isfinite(g2[-150:]).all()) and bool((g2[-150:].float().abs().sum(-1) > 0).all())
