@@ -48,8 +48,9 @@ struct Chunk {
     // elements of vector j that are the array's
     __device__ __forceinline__ bool whole(int j) const { return j * VEC() >= lo && (j + 1) * VEC() <= hi; }
     __device__ __forceinline__ static constexpr int VEC() { return 16 / sizeof(T); }
-    __device__ __forceinline__ uint4 load(int j) const {
-        if (whole(j)) return __ldg(reinterpret_cast<const uint4*>(base) + j);
+    __device__ __forceinline__ uint4 load(int j, bool last = false) const {
+        // (for the last time: not as what no one writes, since a gradient may be scaled in its place)
+        if (whole(j)) return last ? reinterpret_cast<const uint4*>(base)[j] : __ldg(reinterpret_cast<const uint4*>(base) + j);
         uint4 v = {0, 0, 0, 0};
         T* x = reinterpret_cast<T*>(&v);
 #pragma unroll
@@ -170,7 +171,7 @@ __device__ __forceinline__ void scaled(const L& list, int i, int at, float f) {
     const Chunk<T> c(list, i, at);
     uint4 v[CLIP_VECTORS];
 #pragma unroll
-    for (int u = 0; u < CLIP_VECTORS; ++u) v[u] = c.load(u * CLIP_THREADS + threadIdx.x);
+    for (int u = 0; u < CLIP_VECTORS; ++u) v[u] = c.load(u * CLIP_THREADS + threadIdx.x, true);
 #pragma unroll
     for (int u = 0; u < CLIP_VECTORS; ++u) {
         const int j = u * CLIP_THREADS + threadIdx.x;

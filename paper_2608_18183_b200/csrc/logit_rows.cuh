@@ -525,7 +525,8 @@ struct TokenArgs {
     float *loss, *logp, *entropy;             // [rows] or null
     void* grad;              // rows, or null
     float4* stats;           // [rows] or null: m, z (see TokenSums), the mass of the others, what the rounding of logp left
-    int rows, V, ctas, slice, summed;  // summed: logp is for sums over many rows
+    int rows, V, ctas, slice, tiles;  // tiles: slices that a CTA takes in turn (then ctas is 1)
+    int summed;                       // logp is for sums over many rows
     float temperature, low, high, dual, kl, bonus;
     // rows of a scoring forward (see TopkArgs); tokens, logp and entropy are [batch][T] then
     const int2* at;

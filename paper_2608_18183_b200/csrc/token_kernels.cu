@@ -27,6 +27,19 @@ __device__ __forceinline__ void post_sums(const TokenSums& x, TokenSums* slots, 
         if (ENT) post_float(f + 2, ctas, lane, x.a);
     }
 }
+// Sums of two sets of entries.
+template <bool ENT>
+__device__ __forceinline__ TokenSums merged(const TokenSums& x, const TokenSums& y, float c) {
+    TokenSums r = {fmaxf(x.m, y.m), 0.f, 0.f};
+    const auto add = [&](const TokenSums& s) {
+        const float f = rescale(s.m, r.m, c);
+        r.z += s.z * f;
+        if (ENT && f != 0.f) r.a += f * fmaf(s.z, s.m == r.m ? 0.f : (s.m - r.m) * c, s.a);
+    };
+    add(x);
+    add(y);
+    return r;
+}
 // The row's sums from its warps', the same bits in every warp.
 template <bool ENT>
 __device__ __forceinline__ TokenSums collect_sums(const TokenSums* slots, int count, float c) {
@@ -82,7 +95,8 @@ __device__ __forceinline__ float2 policy(const TokenArgs& a, const RowTerms& row
     return {loss, slope};
 }
 
-template <typename T, bool ENT, bool GRAD, int THREADS, int PER_SM>
+// TILED (no gradient): a CTA takes a.tiles slices of a row in turn.
+template <typename T, bool ENT, bool GRAD, bool TILED, int THREADS, int PER_SM>
 __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
     constexpr int G = 16 / sizeof(T), WARPS = THREADS / 32;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -143,12 +157,28 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
             cp_async_wait_all();
             __syncwarp();
             // (one order of the sums, whatever is asked for)
-            TokenSums v = part_sums<ENT>(ss, p, x0, mine, c, [&](auto&& f) {
-                if constexpr (GRAD)
-                    each_of(p, f);
-                else
-                    each_then(p, next, f);
-            });
+            TokenSums v;
+            if constexpr (GRAD) {
+                v = part_sums<ENT>(ss, p, x0, mine, c, [&](auto&& f) { each_of(p, f); });
+            } else if constexpr (!TILED) {
+                v = part_sums<ENT>(ss, p, x0, mine, c, [&](auto&& f) { each_then(p, next, f); });
+            } else {  // a long row tile by tile: nobody looks at it again
+                v = TokenSums::none();
+                for (int tile = 0; tile < a.tiles; ++tile) {
+                    const int at = tile * a.slice, to = at + a.slice;
+                    const T *x = row_at(row) + at, *behind = tile + 1 < a.tiles ? x + a.slice : x1;
+                    const Part<G, WARPS> q(phase_of(x), min(a.slice, a.V - at), wid);
+                    const Part<G, WARPS> q1(phase_of(behind), tile + 1 < a.tiles ? min(a.slice, a.V - to) : n, wid);
+                    Next<T, G, WARPS> then = {ss, behind, q1, tile + 1 < a.tiles || next.more};
+                    if (tile) {
+                        cp_async_wait_all();
+                        __syncwarp();
+                    }
+                    const int place = t - at, in = place >= q.first() - q.P && place < q.last() - q.P ? place : -1;
+                    v = merged<ENT>(v, part_sums<ENT>(ss, q, x, in, c, [&](auto&& f) { each_then(q, then, f); }), c);
+                }
+                next.more = false;
+            }
             const bool alone = WARPS == 1 && a.ctas == 1;  // the warp has the whole row
             if (!alone) {
                 post_sums<ENT, WARPS>(v, slots + parity * places, a.ctas, rank);
@@ -346,24 +376,25 @@ __global__ void __launch_bounds__(SPREAD_THREADS, 4) k_spread_parts(SpreadArgs a
     }
 }
 
-template <typename T, bool ENT, bool GRAD>
+template <typename T, bool ENT, bool GRAD, bool TILED>
 cudaError_t run_token(const TokenArgs& a, Stream& s) {
     const auto bytes = [&](int threads) { return (a.slice + 16) * sizeof(T) + 2 * threads / 32 * a.ctas * sizeof(TokenSums); };
     const auto fit = [&](int threads) { return (int)(227 * 1024 / (bytes(threads) + 1024 + 128)); };  // (1 KB is the system's)
     const auto run = [&](auto threads, auto lanes) {
         constexpr int THREADS = decltype(threads)::value, PER_SM = std::min(32, decltype(lanes)::value / THREADS);
         const size_t smem = bytes(THREADS);
-        cudaError_t e = allow_row_smem<k_token<T, ENT, GRAD, THREADS, PER_SM>>();
+        cudaError_t e = allow_row_smem<k_token<T, ENT, GRAD, TILED, THREADS, PER_SM>>();
         if (e != cudaSuccess) return e;
         int clusters = 0;
-        e = resident_clusters<k_token<T, ENT, GRAD, THREADS, PER_SM>>(a.ctas, THREADS, std::max(1, std::min(PER_SM, fit(THREADS))), smem, a.rows, &clusters);
+        e = resident_clusters<k_token<T, ENT, GRAD, TILED, THREADS, PER_SM>>(a.ctas, THREADS, std::max(1, std::min(PER_SM, fit(THREADS))), smem, a.rows, &clusters);
         if (e != cudaSuccess) return e;
-        return launch_kc(true, k_token<T, ENT, GRAD, THREADS, PER_SM>, dim3((unsigned)clusters * a.ctas), dim3(THREADS), smem, s, a.ctas, a);
+        return launch_kc(true, k_token<T, ENT, GRAD, TILED, THREADS, PER_SM>, dim3((unsigned)clusters * a.ctas), dim3(THREADS), smem, s, a.ctas, a);
     };
     // Threads of a CTA: what a warp does once a row is a good part of its work, so that fewer warps are faster as long as an SM has 24 of
     // them, which is what 80 registers leave room for, beside the rows that its shared memory holds (8192 rows of 16384 fp32 on 512, 256 and
     // 128 threads: 121, 90 and 94 us; with gradients in bf16 134, 109 and 126).
     constexpr std::integral_constant<int, 768> full;
+    if constexpr (TILED) return fit(128) <= 3 ? run(std::integral_constant<int, 256>(), full) : run(std::integral_constant<int, 128>(), full);
     if ((int64_t)a.rows * a.ctas > device_sm_count()) {
         const int f = fit(128);
         if constexpr (GRAD && sizeof(T) == 4) {
@@ -390,8 +421,9 @@ cudaError_t run_token(const TokenArgs& a, Stream& s) {
 
 template <typename T>
 cudaError_t run_token(const TokenArgs& a, bool entropy, Stream& s) {
-    if (a.grad) return entropy ? run_token<T, true, true>(a, s) : run_token<T, false, true>(a, s);
-    return entropy ? run_token<T, true, false>(a, s) : run_token<T, false, false>(a, s);
+    if (a.grad) return entropy ? run_token<T, true, true, false>(a, s) : run_token<T, false, true, false>(a, s);
+    if (a.tiles > 1) return entropy ? run_token<T, true, false, true>(a, s) : run_token<T, false, false, true>(a, s);
+    return entropy ? run_token<T, true, false, false>(a, s) : run_token<T, false, false, false>(a, s);
 }
 
 template <typename T>
@@ -430,7 +462,11 @@ cudaError_t run_spread(const SpreadArgs& args, Stream& s) {
 cudaError_t launch_token(const TokenArgs& args, int rows, int dtype, Stream& s) {
     TokenArgs a = args;
     const RowSplit sp = split_row(rows, a.V, dtype ? 2 : 4, device_sm_count(), SHARED_SM, true);
-    a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice;
+    a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice, a.tiles = 1;
+    // Where nothing is looked at again, long rows are one CTA's, if there are enough of them: no barriers of clusters (8192 rows of 32768 fp32 175 ->
+    // 158 us, 4096 of 65537 217 -> 179).  Not for the
+    // policy's loss, which is to have the same bits with and without its gradient.
+    if (!a.grad && !a.advantage && rows > device_sm_count()) a.tiles = a.ctas, a.ctas = 1;
     const bool entropy = a.entropy || a.d_entropy || a.bonus != 0.f;
     return dtype ? run_token<bf16>(a, entropy, s) : run_token<float>(a, entropy, s);
 }

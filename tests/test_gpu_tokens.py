@@ -343,3 +343,33 @@ def test_places_beyond_32_bits():
     _, want, wsums = binding.hbsjd_preference_loss(x[-300:], t[-300:], small, beta=1e-4)
     torch.testing.assert_close(sums[1:], wsums[1:], rtol=1e-5, atol=1e-4)
     assert bool(torch.isfinite(g2[-150:]).all()) and bool((g2[-150:].float().abs().sum(-1) > 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_long_rows_out_of_the_ordinary(dtype):
+    """More rows than SMs, each longer than a CTA holds: parts without mass, the token in any of them, maxima at either end."""
+    import torch
+    V, rows = 60001, 330
+    x = _rows(7, rows, V, 3.0, dtype, 1)
+    t = sampled(x, 1.0, _gen(7))
+    kind = torch.arange(rows, device="cuda") % 11
+    x[kind == 1, :30000] = NEG
+    x[kind == 2, 20000:] = NEG
+    x[kind == 3] = NEG
+    x[kind == 4] = NEG
+    x[kind == 4, 41234] = 2.0
+    t[kind == 4] = 41234
+    x[kind == 5, 59999] = 60.0
+    x[kind == 6, 3] = 60.0
+    x[kind == 7] -= 5000.0
+    t[kind == 8] = 60000
+    t[kind == 9] = 0
+    t[kind == 10] = -1
+    x[kind == 10] = float("nan")
+    live = kind != 10
+    r = Rows(x[live], t[live], 1.0)
+    logp, H = binding.hbsjd_token_logprobs(x, t)
+    near(logp[live], r.l, r.dl, HALF["fp32"])
+    near(H[live], r.H, r.dH, HALF["fp32"])
+    assert not bool(logp[~live].any()) and not bool(H[~live].any())
+    assert torch.equal(binding.hbsjd_token_logprobs(x, t, want_entropy=False)[0].isinf(), logp.isinf())
