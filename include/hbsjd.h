@@ -485,7 +485,8 @@ int hbsjd_policy_loss(void *cuda_stream, const hbsjd_policy_desc *d, const void 
  *   HBSJD_PREFERENCE_SQUARE   loss = (h - 1 / (2 beta))^2
  *   grad[r] = d (sum over pairs of pair_weight loss) / d logits[r]
  * Pair p is sequences 2 p (chosen) and 2 p + 1 where `interleaved`, else p (chosen) and pairs + p.
- *   offsets   int32 [2 pairs + 1], not decreasing, within 0..rows; else all losses, sums and gradients are NaN
+ *   offsets   int32 [2 pairs + 1], not decreasing, within 0..rows; else all losses, sums and gradients are NaN (but
+ *             of rows whose token is none)
  *   ref_logp  fp32 [rows] or NULL (0);  weight fp32 [rows] or NULL (all 1): 0 leaves a row out;  pair_weight fp32 [pairs] or NULL
  *   loss fp32 [pairs] or NULL;  sums fp32 [2 pairs] or NULL: S_s;  logp fp32 [rows] or NULL: log q_token (0: left out)
  *   grad [rows, V] or NULL: zeros for rows of no sequence

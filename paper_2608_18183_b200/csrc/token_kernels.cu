@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(SPREAD_THREADS, 4) k_spread_parts(SpreadArgs a
             } else if (k.way == 1) {
                 for (int e = lane; e < n; e += 32) {
                     const float q = ex2(held((to_f<T>(x[e]) - k.m) * c)) * k.K;
-                    g[e] = from_f<T>(q == 0.f ? 0.f : q * -k.A * k.scale);
+                    g[e] = from_f<T>(q == 0.f && k.is_number(k.A) ? 0.f : q * -k.A * k.scale);
                 }
             } else if (SHIFTED && P != phase_of(g)) {
                 Shifted<T, G> to(g, 0, n, P);

@@ -192,6 +192,8 @@ struct TokenCoefs {
     float mc, k0, k1;      // others: 2^t (k0 + k1 t), t = x c - mc
     float token;           // the token's gradient
     float m, K, A, B, base, scale;  // one by one: q = K 2^((x - m) c), scale q (B (ln2 t + base) - A)
+    // whether no mass times this factor is none
+    __device__ __forceinline__ bool is_number(float m) const { return m == m && scale == scale; }
     // a (1[v = t] - q_v) + b q_v (log q_v + H), times scale
     template <bool ENT>
     __device__ __forceinline__ void set(const TokenRow& r, const TokenSums& v, float H, float a, float b, float s, float c) {
@@ -313,7 +315,7 @@ __device__ __forceinline__ void part_gradient(const T* ss, const Part<G, WARPS>&
         for (int e = lo + lane; e < hi; e += 32) {
             const float u = held((to_f<T>(ss[p.P + e]) - k.m) * c), q = ex2(u) * k.K;
             const float m = ENT ? fmaf(k.B, fmaf(LN2, u, k.base), -k.A) : -k.A;
-            g[e] = from_f<T>(q == 0.f ? 0.f : q * m * k.scale);
+            g[e] = from_f<T>(q == 0.f && k.is_number(m) ? 0.f : q * m * k.scale);
         }
     } else {
         const f32x2 o = both(-k.mc), c2 = both(c), K0 = both(k.k0), K1 = both(k.k1);

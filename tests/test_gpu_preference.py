@@ -210,3 +210,24 @@ def test_gradients_that_lie_otherwise_than_the_logits(V, pad, shift, dtype):
     _check(x, t, lengths, dtype, beta=0.02)
     grad = torch.empty(407, V + 5, device="cuda", dtype=x.dtype)[:, 3:V + 3]
     _check(x, t, lengths, dtype, beta=0.02, grad=grad)
+
+
+@pytest.mark.parametrize("rows,V", [(40, 3000), (400, 3000), (200, 20011)])
+def test_nan_slopes_reach_every_entry(rows, V):
+    """Offsets that make no sense, and a NaN reference: entries without any share are NaN, too."""
+    import torch
+    x = _rows(1, rows, V) * 40
+    x[:, ::7] = NEG
+    for dtype in (torch.float32, torch.bfloat16):
+        y = x.to(dtype)
+        t = torch.ones(rows, dtype=torch.int32, device="cuda")
+        for pad in (0, 1):
+            grad = torch.empty(rows, V + pad, device="cuda", dtype=dtype)[:, :V]
+            g = binding.hbsjd_preference_loss(y, t, torch.tensor([0, 9, 3], device="cuda").int(), grad=grad)[1]
+            assert bool(torch.isnan(g).all())
+            ref = torch.zeros(rows, device="cuda")
+            ref[3] = float("nan")
+            half = torch.tensor([0, 10, 20, 30, 40], device="cuda").int()
+            loss, g, _ = binding.hbsjd_preference_loss(y, t, half, ref, interleaved=True, grad=grad)
+            assert bool(torch.isnan(loss[0])) and bool(torch.isfinite(loss[1]))
+            assert bool(torch.isnan(g[:20]).all()) and bool(torch.isfinite(g[20:]).all())

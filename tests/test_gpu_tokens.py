@@ -373,3 +373,19 @@ def test_long_rows_out_of_the_ordinary(dtype):
     near(H[live], r.H, r.dH, HALF["fp32"])
     assert not bool(logp[~live].any()) and not bool(H[~live].any())
     assert torch.equal(binding.hbsjd_token_logprobs(x, t, want_entropy=False)[0].isinf(), logp.isinf())
+
+
+def test_nan_advantages_and_weights_reach_every_entry():
+    import torch
+    x, t = _rows(1, 6, 3000) * 40, torch.ones(6, dtype=torch.int32, device="cuda")
+    x[:, ::7] = NEG
+    one = torch.ones(6, device="cuda")
+    bad = one.clone()
+    bad[2] = float("nan")
+    for call in (lambda ent: binding.hbsjd_policy_loss(x, t, bad, entropy=ent), lambda ent: binding.hbsjd_policy_loss(x, t, one, bad, entropy=ent),
+                 lambda ent: binding.hbsjd_policy_loss(x, t, one, weight=bad, entropy=ent),
+                 lambda ent: binding.hbsjd_policy_loss(x, t, one, ref_logp=bad, kl=0.1, entropy=ent)):
+        for ent in (0.0, 0.1):
+            g = call(ent)[1]
+            # (against a reference of e^1, tokens of e^-400 have slopes beyond fp32: infinite, no NaN)
+            assert bool(torch.isnan(g[2]).all()) and not bool(torch.isnan(g[[0, 1, 3, 4, 5]]).any())
