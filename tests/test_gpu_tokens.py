@@ -389,3 +389,39 @@ def test_nan_advantages_and_weights_reach_every_entry():
             g = call(ent)[1]
             # (against a reference of e^1, tokens of e^-400 have slopes beyond fp32: infinite, no NaN)
             assert bool(torch.isnan(g[2]).all()) and not bool(torch.isnan(g[[0, 1, 3, 4, 5]]).any())
+
+
+def test_host_threads_and_streams_at_once():
+    import threading
+    import torch
+    x, t = _rows(1, 333, 5001), torch.randint(0, 5001, (333,), generator=_gen(1), device="cuda").int()
+    A, offsets = torch.randn(333, generator=_gen(2), device="cuda"), torch.tensor([0, 100, 150, 300, 333], device="cuda").int()
+    arrays = [torch.randn(n, generator=_gen(n), device="cuda") for n in (100000, 33, 70001)]
+    outs = [torch.empty_like(v) for v in arrays]
+
+    def calls(out):
+        p = binding.hbsjd_policy_loss(x, t, A, entropy=0.01)
+        q = binding.hbsjd_preference_loss(x, t, offsets)
+        n = binding.hbsjd_clip_gradients(arrays, 3.0, out=out)
+        return [*p[:3], *q, *binding.hbsjd_token_logprobs(x, t), n, *out]
+
+    want = [v.clone() for v in calls(outs)]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work():
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            own = [torch.empty_like(v) for v in arrays]
+            for _ in range(30):
+                got = calls(own)
+                if not all(torch.equal(a, b) for a, b in zip(got, want)):
+                    wrong.append(1)
+            stream.synchronize()
+
+    threads = [threading.Thread(target=work) for _ in range(4)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not wrong
