@@ -6,7 +6,7 @@
 //
 // A row's gradient needs its whole pair's sums, so the call is three kernels: k_token sums over the rows and keeps 16 bytes of each, k_pairs (here,
 // 5 us of latencies) makes the slopes, k_spread writes the gradient from what was kept, reading the logits a second time, the last rows
-// first.  That second reading is what bounds it: 16 pairs of 256 positions of 16384 fp32 250 us, where two readings and a writing take 229 at a
+// first.  That second reading is what bounds it: 16 pairs of 256 positions of 16384 fp32 246 us, where two readings and a writing take 229 at a
 // copy's rate (one reading 156).  L2 does not save it: a pair is 33 MB there, and gradients some rows behind the sums, in one kernel, still read 0.92
 // of all logits twice (350 us); batches of fewer pairs a launch pay 5 us of ramp each.
 #include "../../include/hbsjd.h"
