@@ -13,7 +13,6 @@ namespace hbsjd {
 
 constexpr int MAX_LOGIT_V = 131072;    // entries of a row: what eight CTAs hold of two fp32 rows
 constexpr int MAX_LISTED = 1024;       // entries of a top-K list
-constexpr int ROW_CTAS = 8;            // CTAs of a row, at most (the portable cluster size)
 constexpr int ROW_SMEM = 216 * 1024;   // dynamic shared memory that a CTA may ask for
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
@@ -464,20 +463,6 @@ inline cudaError_t resident_clusters(int ctas, int threads, int per_sm, size_t s
     if (most > 0) *clusters = std::min(*clusters, most);
     return cudaSuccess;
 }
-
-// How a row is split: CTAs (a cluster, where more than one) and the elements that each holds.
-struct RowSplit {
-    int ctas, slice;
-};
-// 72 KB a CTA, so that three share an SM; parts of 4096 entries and more where there are SMs to spare, if `spread` (a row of 16384
-// fp32 on 1, 2, 4, 8 CTAs: divergence with gradient 6.0, 6.0, 4.8, 4.3 us, from a list of 64 8.8, 7.9, 6.9, 6.7; one of 4096 is fastest on one).
-inline RowSplit split_row(int64_t rows, int V, int bytes_per_element, int sms, int most_bytes, bool spread) {
-    int ctas = 1;
-    while (ctas < ROW_CTAS && (int64_t)V * bytes_per_element > (int64_t)most_bytes * ctas) ctas *= 2;
-    while (spread && ctas < ROW_CTAS && rows * ctas * 2 <= sms && V > 4096 * ctas) ctas *= 2;
-    return {ctas, ((V + ctas - 1) / ctas + 7) / 8 * 8};
-}
-constexpr int SHARED_SM = 72 * 1024;
 
 struct DistillArgs {
     const void *s, *t;       // student's and teacher's rows

@@ -165,11 +165,12 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
             } else {  // a long row tile by tile: nobody looks at it again
                 v = TokenSums::none();
                 for (int tile = 0; tile < a.tiles; ++tile) {
-                    const int at = tile * a.slice, to = at + a.slice;
-                    const T *x = row_at(row) + at, *behind = tile + 1 < a.tiles ? x + a.slice : x1;
-                    const Part<G, WARPS> q(phase_of(x), min(a.slice, a.V - at), wid);
-                    const Part<G, WARPS> q1(phase_of(behind), tile + 1 < a.tiles ? min(a.slice, a.V - to) : n, wid);
-                    Next<T, G, WARPS> then = {ss, behind, q1, tile + 1 < a.tiles || next.more};
+                    const bool last = tile + 1 == a.tiles;
+                    const int at = tile * a.slice;
+                    const T *x = row_at(row) + at, *behind = last ? x1 : x + a.slice;
+                    const auto q = tile_part<G, WARPS>(phase_of(x), a.V, a.slice, tile, wid);
+                    const auto q1 = tile_part<G, WARPS>(phase_of(behind), a.V, a.slice, last ? 0 : tile + 1, wid);
+                    Next<T, G, WARPS> then = {ss, behind, q1, !last || next.more};
                     if (tile) {
                         cp_async_wait_all();
                         __syncwarp();
