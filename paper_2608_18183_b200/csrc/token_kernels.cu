@@ -29,10 +29,10 @@ __device__ __forceinline__ void post_sums(const TokenSums& x, TokenSums* slots, 
 }
 // Sums of two sets of entries.
 template <bool ENT>
-__device__ __forceinline__ TokenSums merged(const TokenSums& x, const TokenSums& y, float c) {
+__device__ __forceinline__ TokenSums merged(const TokenSums& x, const TokenSums& y, float c, bool summed) {
     TokenSums r = {fmaxf(x.m, y.m), 0.f, 0.f};
     const auto add = [&](const TokenSums& s) {
-        const float f = rescale(s.m, r.m, c);
+        const float f = summed ? rescale_without_lean(s.m, r.m, c) : rescale(s.m, r.m, c);
         r.z += s.z * f;
         if (ENT && f != 0.f) r.a += f * fmaf(s.z, s.m == r.m ? 0.f : (s.m - r.m) * c, s.a);
     };
@@ -42,14 +42,14 @@ __device__ __forceinline__ TokenSums merged(const TokenSums& x, const TokenSums&
 }
 // The row's sums from its warps', the same bits in every warp.
 template <bool ENT>
-__device__ __forceinline__ TokenSums collect_sums(const TokenSums* slots, int count, float c) {
+__device__ __forceinline__ TokenSums collect_sums(const TokenSums* slots, int count, float c, bool summed) {
     const int lane = threadIdx.x & 31;
     TokenSums r = TokenSums::none();
     for (int j = lane; j < count; j += 32) r.m = fmaxf(r.m, slots[j].m);
     r.m = max_of_warp(r.m);
     for (int j = lane; j < count; j += 32) {
         const TokenSums s = slots[j];
-        const float f = rescale(s.m, r.m, c);
+        const float f = summed ? rescale_without_lean(s.m, r.m, c) : rescale(s.m, r.m, c);
         r.z += s.z * f;
         if (ENT && f != 0.f) r.a += f * fmaf(s.z, s.m == r.m ? 0.f : (s.m - r.m) * c, s.a);
     }
@@ -128,6 +128,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
     const auto logit_of = [&](int row, int t) { return t < 0 ? 0.f : to_f<T>(row_at(row)[t]); };
     const auto part_of = [&](const T* x) { return Part<G, WARPS>(phase_of(x), n, wid); };
     const int64_t stride = (int64_t)step * a.ld;
+    const bool summed = !ENT && !GRAD && a.summed;  // (the preference loss asks for no entropies)
     int row = blockIdx.x / a.ctas, parity = 0;
     int t = token_of(row), t1 = token_of(row + step);
     float xt = logit_of(row, t);
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
                         __syncwarp();
                     }
                     const int place = t - at, in = place >= q.first() - q.P && place < q.last() - q.P ? place : -1;
-                    v = merged<ENT>(v, part_sums<ENT>(ss, q, x, in, c, [&](auto&& f) { each_then(q, then, f); }), c);
+                    v = merged<ENT>(v, part_sums<ENT>(ss, q, x, in, c, [&](auto&& f) { each_then(q, then, f); }), c, summed);
                 }
                 next.more = false;
             }
@@ -188,8 +189,8 @@ __global__ void __launch_bounds__(THREADS, PER_SM) k_token(TokenArgs a) {
             }
             TokenCoefs k;
             if (GRAD || wid == 0) {  // (each warp for itself: one for all, and a barrier, cost 16384 rows of 16384 365 us in place of 351)
-                if (!alone) v = collect_sums<ENT>(slots + (parity ^ 1) * places, places, c);
-                const TokenRow r(v, xt, inv_tau, !GRAD && a.summed);
+                if (!alone) v = collect_sums<ENT>(slots + (parity ^ 1) * places, places, c, summed);
+                const TokenRow r(v, xt, inv_tau, summed);
                 float H = 0.f;
                 if (ENT && !r.empty) H = (v.z == 0.f || r.qo == 0.f ? 0.f : r.qo * (r.Lk - LN2 * __fdividef(v.a, v.z))) - (r.qt == 0.f ? 0.f : r.qt * r.l);
                 float2 f = {0.f, 0.f};

@@ -66,15 +66,27 @@ __device__ __forceinline__ float2 ln(float z) {
     return {hi, f + fmaf((float)k, LN2, -hi) - (float)k * 1.90465e-9f};  // (LN2 is that much above ln 2)
 }
 // The same for sums over many rows, where what all rows are off alike adds up (lg2 leaves up to 2e-8 a row, by its argument): z = 2^k f with
-// f in [sqrt 1/2, sqrt 2), and ln f = 2 (u + u^3 / 3 + u^5 / 5 ...) with u = (f - 1) / (f + 1), which leaves 1e-9 behind u^9; and the 2e-8 that sums of
-// ex2 were below their exact ones (1e-8 of 1000 entries, 3e-8 of 16384).
+// f in [sqrt 1/2, sqrt 2), and ln f = 2 (u + u^3 / 3 + u^5 / 5 ...) with u = (f - 1) / (f + 1), which leaves 1e-9 behind u^9.
 __device__ __forceinline__ float2 ln_without_lean(float z) {
     const int b = __float_as_int(z);
     if ((uint32_t)(b - 0x00800000) >= 0x7f000000u) return ln(z);  // zero, infinities and NaN
     const int k = (b - 0x3f3504f3) >> 23;  // (sqrt 1/2)
     const float f = __int_as_float(b - (k << 23)), u = __fdividef(f - 1.f, f + 1.f), u2 = u * u;
     const float g = 2.f * u * fmaf(u2, fmaf(u2, fmaf(u2, fmaf(u2, 1.f / 9, 1.f / 7), 0.2f), 1.f / 3), 1.f), hi = (float)k * LN2;
-    return {hi, g + (fmaf((float)k, LN2, -hi) - (float)k * 1.90465e-9f + 2e-8f)};
+    return {hi, g + (fmaf((float)k, LN2, -hi) - (float)k * 1.90465e-9f)};
+}
+// rescale for such sums.  ex2 is exact at whole numbers and 5e-8 below 2^x on average elsewhere: sums that are brought from a warp's reference to
+// the row's, or from a tile's, would lean by as much each time.  2^p = 2^i e^y with |y| <= ln2 / 2; the series leaves 5e-9 behind y^7.
+// (What is left of it is in the entries: l is up to 5e-8 times the others' mass too high on average, and the rounding of c, at a temperature of 1 1.3e-8
+// of their mean distance from the largest, takes from that.  Of 2 to 131072 normal logits with a deviation of 0.1 to 10: a mean of -3e-8 to 3e-8
+// a row; where all others are alike, none.)
+__device__ __forceinline__ float rescale_without_lean(float from, float to, float c) {
+    if (from == -INFINITY) return 0.f;
+    if (from == to) return 1.f;
+    const float p = (from - to) * c, i = rintf(p), y = (p - i) * LN2;
+    if (!(i >= -126.f)) return 0.f;
+    const float e = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.f / 5040, 1.f / 720), 1.f / 120), 1.f / 24), 1.f / 6), 0.5f), 1.f), 1.f);
+    return e * __int_as_float(((int)i + 127) << 23);
 }
 
 // log(1 + s), s in 0..1, to its own last digits: 2 (u + u^3 / 3 + u^5 / 5 ...) with u = s / (2 + s), which leaves 1e-8 of it behind u^15.
