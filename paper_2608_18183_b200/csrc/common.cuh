@@ -17,11 +17,11 @@ typedef __nv_bfloat16 bf16;
 // tail.  Most trigger after their own wait ("late"): triggered before it, a third kernel's CTAs take the shared memory
 // that the second's would have had (one L image 0.94 times the time with the gate/up projection late, 24 L images token
 // by token 0.99, four tiny images 0.99 with the small kernels late).
-// All that precedes a late kernel is complete when the next one starts.  Four kernels use that: the QKV projection (rows,
-// pages and rotations), attention (work list, pages, old keys), the accept kernel behind an LM head and k_commit read what
-// kernels before their predecessor have written before their own wait, through L2.  Else nothing before pdl_wait() touches
-// global memory that any kernel writes.  Stream carries which kind the last kernel was: the launchers of these four hand it
-// to the kernel, which waits first behind a kernel that triggers early.
+// All that precedes a late kernel is complete when the next one starts.  Five kernels use that: the QKV projection (rows,
+// pages and rotations), attention (work list, pages, old keys), the accept kernel behind an LM head, k_commit and k_pairs (the
+// sequences' offsets) read what kernels before their predecessor have written before their own wait, through L2.  Else nothing
+// before pdl_wait() touches global memory that any kernel writes.  Stream carries which kind the last kernel was: the launchers
+// of these five hand it to the kernel, which waits first behind a kernel that triggers early.
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -540,6 +540,7 @@ struct PairArgs {
     float *loss, *sums;      // [pairs], [2 pairs]; null: not wanted
     float* slope;            // [rows] or null
     int rows, V, pairs, kind, interleaved;
+    bool early;              // the kernel before triggers late (see pdl_wait)
     float beta, smoothing, margin;
 };
 // directly behind launch_token, which makes logp

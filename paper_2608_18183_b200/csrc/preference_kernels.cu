@@ -32,35 +32,40 @@ __device__ __forceinline__ double2 pair_loss(const PairArgs& a, double h) {
             a.beta * (e * up - (1.0 - e) * down)};
 }
 
-// A CTA a pair (or several in turn: each looks at all offsets), half of it a sequence.  What it reads of the caller's before it waits for the kernel in front was there before that one
-// began (see pdl_wait): the rows' log-probabilities are all that comes from it.
+// A CTA a pair (or several in turn: each looks at all offsets), half of it a sequence.  The offsets are the caller's and nothing of the kernel in front:
+// behind one that triggers late they are read before the wait (see pdl_wait).
 __global__ void __launch_bounds__(PAIR_THREADS) k_pairs(PairArgs a) {
     constexpr int HALF = PAIR_THREADS / 2;
     __shared__ double parts[PAIR_THREADS / 32];
     const int tid = threadIdx.x, side = tid / HALF;
     // offsets that decrease, or leave the rows: nothing is known of any sequence
     bool wrong = false;
+    if (!a.early) pdl_wait();
     for (int i = tid; i <= 2 * a.pairs; i += PAIR_THREADS) {
-        const int at = __ldg(a.offsets + i), before = i ? __ldg(a.offsets + i - 1) : 0;
+        const int at = __ldcg(a.offsets + i), before = i ? __ldcg(a.offsets + i - 1) : 0;
         wrong |= at < before || at > a.rows;
     }
-    const int from = __ldg(a.offsets), to = __ldg(a.offsets + 2 * a.pairs);
+    const int from = __ldcg(a.offsets), to = __ldcg(a.offsets + 2 * a.pairs);
+    const auto sequence = [&](int pair, bool rejected) { return a.interleaved ? 2 * pair + rejected : rejected ? a.pairs + pair : pair; };
+    // rows of the first pair's sequence (read here, else they are another read from L2 behind the wait)
+    int2 rows = {__ldcg(a.offsets + sequence(blockIdx.x, side)), __ldcg(a.offsets + sequence(blockIdx.x, side) + 1)};
+    pdl_wait();
+    pdl_trigger();
     // a row's weight; 0: it is left out
     const auto weight = [&](int r) {
         const int t = __ldg(a.tokens + r);
         return t < 0 || t >= a.V ? 0.f : a.weight ? __ldg(a.weight + r) : 1.f;
     };
-    pdl_wait();
-    pdl_trigger();
     wrong = __syncthreads_or(wrong);
     for (int pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
-        const int chosen = a.interleaved ? 2 * pair : pair, other = a.interleaved ? 2 * pair + 1 : a.pairs + pair;
+        const int chosen = sequence(pair, false), other = sequence(pair, true);
         if (wrong) {
             if (tid == 0 && a.loss) a.loss[pair] = NAN;
             if (tid == 0 && a.sums) a.sums[chosen] = a.sums[other] = NAN;
             continue;
         }
-        const int seq = side ? other : chosen, begin = __ldg(a.offsets + seq) + tid % HALF, end = __ldg(a.offsets + seq + 1);
+        if (pair != blockIdx.x) rows = {__ldcg(a.offsets + (side ? other : chosen)), __ldcg(a.offsets + (side ? other : chosen) + 1)};
+        const int begin = rows.x + tid % HALF, end = rows.y;
         double v = 0.0;
 #pragma unroll 4
         for (int r = begin; r < end; r += HALF) {
@@ -97,7 +102,9 @@ __global__ void __launch_bounds__(PAIR_THREADS) k_pairs(PairArgs a) {
 
 }  // namespace
 
-cudaError_t launch_pairs(const PairArgs& a, Stream& s) {
+cudaError_t launch_pairs(const PairArgs& args, Stream& s) {
+    PairArgs a = args;
+    a.early = s.late;
     return launch_k(k_pairs, dim3((unsigned)std::min(a.pairs, 4 * device_sm_count())), dim3(PAIR_THREADS), 0, s, a);
 }
 
