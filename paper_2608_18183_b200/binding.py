@@ -516,9 +516,11 @@ def hbsjd_policy_loss(logits, tokens, advantage, old_logp=None, ref_logp=None, w
 
 
 def hbsjd_preference_loss(logits, tokens, offsets, ref_logp=None, weight=None, pair_weight=None, temperature=1.0, beta=0.1,
-                          kind="sigmoid", smoothing=0.0, margin=0.0, interleaved=False, want_grad=True, grad=None, stream=None):
+                          kind="sigmoid", smoothing=0.0, margin=0.0, interleaved=False, want_grad=True, grad=None, stream=None,
+                          want_logp=False):
     """The loss of pairs of sequences, one preferred to the other, and its gradient in the logits: (loss fp32 [pairs], grad like
-    logits or None, sums fp32 [2 pairs]: weight (logp - ref_logp) summed over each sequence).  Sequence s is rows offsets[s] ..
+    logits or None, sums fp32 [2 pairs]: weight (logp - ref_logp) summed over each sequence), and with want_logp behind them the tokens'
+    log-probabilities, fp32 [rows] (0: left out), for a likelihood term beside it.  Sequence s is rows offsets[s] ..
     offsets[s + 1] - 1 (int32 [2 pairs + 1]); the chosen ones are the even ones if interleaved, else the first half.  ref_logp, weight
     fp32 [rows], pair_weight fp32 [pairs] or None.  kind: "sigmoid", "hinge" or "square" (see include/hbsjd.h).  grad: as in
     hbsjd_distill."""
@@ -528,7 +530,7 @@ def hbsjd_preference_loss(logits, tokens, offsets, ref_logp=None, weight=None, p
     if stream is not None or device.index != _torch.cuda.current_device():
         return _elsewhere(hbsjd_preference_loss, what, logits, stream,
                           (logits, tokens, offsets, ref_logp, weight, pair_weight, temperature, beta, kind, smoothing, margin, interleaved,
-                           want_grad, grad), {})
+                           want_grad, grad, None, want_logp), {})
     rows, V = logits.shape
     t, f32 = _tokens(what, tokens, device, rows), _torch.float32
     if kind not in PREFERENCE:
@@ -543,16 +545,18 @@ def hbsjd_preference_loss(logits, tokens, offsets, ref_logp=None, weight=None, p
     given = grad is not None
     grad, g, ld_g = _gradient(what, grad, want_grad, logits)
     loss, sums = logits.new_empty((pairs,), dtype=f32), logits.new_empty((2 * pairs,), dtype=f32)
+    logp = logits.new_empty((rows,), dtype=f32) if want_logp else None
     if not rows:
         _refuse(what, "sequences without a row")
     d = hbsjd_preference_desc(rows, V, dtype, pairs, PREFERENCE[kind], 1 if interleaved else 0, ld, ld_g, temperature, beta, smoothing,
                               margin)
     L = load()
     work = logits.new_empty((L.hbsjd_preference_workspace(d),), dtype=_torch.uint8)
-    _call(what, L.hbsjd_preference_loss, device, d, x, t, at, ref, w, pw, work.data_ptr(), loss.data_ptr(), sums.data_ptr(), None, g)
+    _call(what, L.hbsjd_preference_loss, device, d, x, t, at, ref, w, pw, work.data_ptr(), loss.data_ptr(), sums.data_ptr(),
+          logp.data_ptr() if want_logp else None, g)
     if given:
         _torch.autograd.graph.increment_version(grad)
-    return loss, grad, sums
+    return (loss, grad, sums, logp) if want_logp else (loss, grad, sums)
 
 
 def _dense(x):
