@@ -1,4 +1,4 @@
-// C entries of the operators on rows of logits (see include/hbsjd.h): checks of arguments, then one launch.
+// C entries of the operators on rows of logits (see include/hbsjd.h): checks of arguments, then one launch (three for the preference loss, two and more for clipping).
 #include <cstdarg>
 #include <cstdio>
 

@@ -8,7 +8,8 @@
 // next row group by group as it reads this one for the last time, wherever that row lies behind 16 bytes.  Long rows, and few, are split over a
 // cluster.  Measured, the kernel alone: log-probabilities and entropies of 8192 rows of 16384 fp32 88 us (0.94 of a copy's rate); policy
 // loss with gradient of 16384 such rows, an eighth left out, 327 us (0.95); with entropy, 8192 rows in bf16 110 us (0.75); backward of 3001 rows of 24001 bf16 70 us
-// (0.64: rows that begin anywhere in a line cost a quarter more requests).
+// (0.63, as at whole turns and with aligned rows: four rows fit an SM, whose latencies leave issue slots and exponentials half idle).  Warps whose
+// part of a row begins with a stretch of -inf go entry by entry: a third of the row masked takes two to four times as long.
 #include <type_traits>
 
 #include "token_rows.cuh"
@@ -468,7 +469,7 @@ cudaError_t launch_token(const TokenArgs& args, int rows, int dtype, Stream& s) 
     const RowSplit sp = split_row(rows, a.V, dtype ? 2 : 4, device_sm_count(), SHARED_SM, true);
     a.rows = rows, a.ctas = sp.ctas, a.slice = sp.slice, a.tiles = 1;
     // Where nothing is looked at again, long rows are one CTA's, if there are enough of them: no barriers of clusters (8192 rows of 32768 fp32 175 ->
-    // 158 us, 4096 of 65537 217 -> 179).  Not for the
+    // 158 us, 4096 of 65537 217 -> 181).  Not for the
     // policy's loss, which is to have the same bits with and without its gradient.
     if (!a.grad && !a.advantage && rows > device_sm_count()) a.tiles = a.ctas, a.ctas = 1;
     const bool entropy = a.entropy || a.d_entropy || a.bonus != 0.f;
