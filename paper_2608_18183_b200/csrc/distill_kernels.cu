@@ -35,7 +35,7 @@ constexpr float NEAR = 1.f / 64;
 // An outcome's p (e^r - 1 - r) and q (e^-r - 1 + r), r = log q / p, of any size: those far from one another as they are; no mass on either
 // side: r is not looked at.
 __device__ __forceinline__ float2 near_terms(float p, float q, float r) {
-    if (fabsf(r) < 0.75f) {  // series over r^2 / 2, whose next terms are below 7e-7 of them
+    if (fabsf(r) < 0.75f) {  // series over r^2 / 2, whose next terms are below 7e-7 of the one and 9e-7 of the other
         const float r2 = r * r, even = fmaf(r2, fmaf(r2, fmaf(r2, 1.f / 40320, 1.f / 720), 1.f / 24), 0.5f);
         const float odd = r * fmaf(r2, fmaf(r2, 1.f / 5040, 1.f / 120), 1.f / 6);
         return {p * r2 * (even + odd), q * r2 * (even - odd)};
